@@ -317,6 +317,168 @@ painn_status painn_trainer_step(painn_trainer* tr, const painn_graph* graph, con
 painn_status painn_trainer_params(const painn_trainer* tr, int64_t* n_params, double* params, double* grad);
 painn_status painn_trainer_free(painn_trainer* tr);
 
+/* ---- tuning heads: operators in FP32 and BF16 ------------------------------ */
+
+/* The operators that a program needs to tune heads or an adapter in FP32 or
+ * BF16 on the features of an encoder that stays as it is (section
+ * "Precision-sensitivity characterization at inference and fine-tuning
+ * stage"): layer norm, the dense layer with its epilogue, the dense layer
+ * grouped by dataset head, each with its reverse pass, and AdamW over many
+ * tensors.  FP64 is refused (PAINN_E_UNSUPPORTED): painn_trainer_* trains
+ * whole models in FP64.
+ *
+ * Matrices are row-major with contiguous rows and a row stride in elements
+ * (ld >= row width).  Any alignment to the element is accepted.  An output
+ * must not overlap an input unless said.  Sums, statistics and products
+ * accumulate in FP32; BF16 outputs are rounded once, to nearest even.
+ * Deterministic: no reduction's order depends on timing.  Every call is
+ * asynchronous on the context's stream.  The reverse passes keep partial
+ * sums in a workspace of the context (calls on one context that run on
+ * different streams must be ordered by the caller); a call that has to enlarge
+ * it while the stream is being captured is refused with PAINN_E_OOM (run the
+ * call once before the capture, and no larger one while the graph is in
+ * use). */
+
+/* y = (x - mean) rstd gamma + beta for every row of x [rows, cols], mean the
+ * row's mean and rstd = 1 / sqrt(variance + eps) (the variance over cols,
+ * not cols - 1).  gamma, beta [cols] in the precision's type; mean, rstd
+ * [rows] FP32 outputs (either may be NULL).  y may be x.
+ * Errors: PAINN_E_ARG (null pointers, cols < 1, rows < 0, a stride below
+ * cols, eps not finite or < 0), PAINN_E_UNSUPPORTED (FP64). */
+painn_status painn_layer_norm(painn_ctx* ctx, painn_precision precision, int64_t rows, int32_t cols,
+                              const void* x, int64_t ldx, const void* gamma, const void* beta, double eps,
+                              void* y, int64_t ldy, float* mean, float* rstd);
+/* Its reverse pass, from dy = dL/dy and the forward's mean and rstd: dx, and
+ * dgamma, dbeta [cols] summed over the rows (zero for no rows).  dx may be
+ * NULL (not wanted) or dy; dgamma and dbeta may both be NULL.  Errors as
+ * painn_layer_norm; PAINN_E_OOM. */
+painn_status painn_layer_norm_backward(painn_ctx* ctx, painn_precision precision, int64_t rows, int32_t cols,
+                                       const void* dy, int64_t lddy, const void* x, int64_t ldx,
+                                       const void* gamma, const float* mean, const float* rstd, void* dx,
+                                       int64_t lddx, void* dgamma, void* dbeta);
+
+typedef enum {
+  PAINN_ACT_NONE = 0,        /* z */
+  PAINN_ACT_SILU = 1,        /* z / (1 + exp(-z)) */
+  PAINN_ACT_RELU = 2,        /* max(z, 0) */
+  PAINN_ACT_GELU = 3         /* z (1 + erf(z / sqrt 2)) / 2 */
+} painn_activation;
+
+/* A dense layer: z = x w^T + bias, y = activation(z) + residual. */
+typedef struct {
+  int32_t precision;         /* painn_precision: PAINN_FP32 or PAINN_BF16 */
+  int32_t activation;        /* painn_activation */
+  int64_t rows;
+  int32_t d_in, d_out;
+  const void* x;             /* [rows, d_in] */
+  int64_t ldx;
+  const void* w;             /* [d_out, d_in], contiguous */
+  const void* bias;          /* [d_out], or NULL */
+  const void* residual;      /* [rows, d_out], or NULL; may be y with y's stride */
+  int64_t ldr;
+  void* y;                   /* [rows, d_out] */
+  int64_t ldy;
+  void* z;                   /* [rows, d_out] pre-activations for the reverse pass, or NULL */
+  int64_t ldz;
+} painn_linear_args;
+
+/* Its reverse pass: dz = dy activation'(z), dx = dz w, dw = dz^T x, dbias =
+ * the sum of dz over the rows.  With xz, the pre-activations that x =
+ * x_activation(xz) came from, dx is the gradient of xz: (dz w)
+ * x_activation'(xz), in the same pass.  The residual's gradient is dy.  In
+ * BF16 dz is rounded to BF16 before the products where there is an
+ * activation.  relu'(0) = 0. */
+typedef struct {
+  int32_t precision, activation;
+  int64_t rows;
+  int32_t d_in, d_out;
+  const void* dy;            /* [rows, d_out] */
+  int64_t lddy;
+  const void* z;             /* [rows, d_out] the forward's z; not read for PAINN_ACT_NONE */
+  int64_t ldz;
+  const void* x;             /* [rows, d_in]; read for dw only */
+  int64_t ldx;
+  const void* w;             /* [d_out, d_in]; read for dx only */
+  const void* xz;            /* [rows, d_in]; not read for x_activation PAINN_ACT_NONE */
+  int64_t ldxz;
+  int32_t x_activation;
+  int32_t reserved;          /* 0 */
+  void* dx;                  /* [rows, d_in], or NULL; may be xz with xz's stride */
+  int64_t lddx;
+  void* dw;                  /* [d_out, d_in], or NULL */
+  void* dbias;               /* [d_out], or NULL; needs dw */
+} painn_linear_backward_args;
+
+/* args is a host pointer.  Errors: PAINN_E_ARG (null pointers, widths < 1,
+ * rows < 0, a stride below the row's width, an unknown activation, dbias
+ * without dw), PAINN_E_UNSUPPORTED (FP64; widths above 2^20; more than 2^31
+ * tiles), PAINN_E_OOM (the reverse pass's workspace). */
+painn_status painn_linear(painn_ctx* ctx, const painn_linear_args* args);
+painn_status painn_linear_backward(painn_ctx* ctx, const painn_linear_backward_args* args);
+
+/* The same with one weight matrix per group of consecutive rows, as the
+ * per-dataset heads need: w and dw are [n_groups, d_out, d_in], bias and
+ * dbias [n_groups, d_out], and group g has the rows [offsets[g],
+ * offsets[g+1]) (offsets [n_groups + 1] int32, device, non-decreasing within
+ * [0, rows]; entries outside are taken as the nearest bound).  A group may be
+ * empty: its dw and dbias are zero.  Rows of no group are not written and do
+ * not count.  1 <= n_groups <= 4096, rows < 2^31.  Errors as painn_linear. */
+painn_status painn_grouped_linear(painn_ctx* ctx, const painn_linear_args* args, int32_t n_groups,
+                                  const int32_t* offsets);
+painn_status painn_grouped_linear_backward(painn_ctx* ctx, const painn_linear_backward_args* args,
+                                           int32_t n_groups, const int32_t* offsets);
+
+/* AdamW over many tensors in one launch: FP32 parameters, FP32 or BF16
+ * gradients, an optional BF16 copy of the parameters for the products, states
+ * in FP32 or 8 bits.  With t the number of the step,
+ *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
+ *   p = p (1 - lr weight_decay) - lr / (1 - beta1^t) m
+ *         / (sqrt(v) / sqrt(1 - beta2^t) + eps),
+ * in FP32, each operation rounded as written.  In 8 bits a state's value is a
+ * code times a scale: m and sqrt(v) as e4m3 codes (OCP 8-bit floats: 4
+ * exponent bits, 3 fraction bits, largest value 448), one FP32 scale for 256
+ * consecutive values of a tensor, the largest magnitude / 448, so that the
+ * largest is exact to 2^-4 of itself and values down to 4e-6 of it are kept.
+ * A second moment above zero never gets the code of zero: a denominator that
+ * vanished beside a first moment that did not would make a step without
+ * bound.  The step uses the states before they are coded.  An infinity or NaN
+ * in a block's gradients makes the block's states NaN from then on. */
+typedef struct {
+  int64_t n;                 /* values, >= 0 */
+  float* param;              /* [n] */
+  const void* grad;          /* [n], grad_precision */
+  void* copy;                /* [n] BF16, or NULL */
+  void* m;                   /* [n] FP32, or e4m3 codes of m */
+  void* v;                   /* [n] FP32, or e4m3 codes of sqrt(v) */
+  float* m_scale;            /* 8 bits: [ceil(n / 256)]; else not read */
+  float* v_scale;
+} painn_adamw_tensor;
+typedef struct {
+  double beta1, beta2;       /* in [0, 1) */
+  double eps;                /* > 0 */
+  double weight_decay;       /* >= 0 */
+  int32_t state_bits;        /* 8 or 32 */
+  int32_t grad_precision;    /* PAINN_FP32 or PAINN_BF16 */
+  int64_t steps;             /* steps already made with these states */
+} painn_adamw_config;
+typedef struct painn_adamw painn_adamw;
+
+/* Create the optimizer of n_tensors tensors (host arrays tensors and cfg).
+ * The parameters, gradients and states stay the caller's, are read and
+ * written in place by every step, and must live as long as the optimizer;
+ * states of zeros (8 bits: zero codes and scales) start a run.  Synchronises
+ * the stream.  Errors: PAINN_E_ARG (null pointers, values out of range),
+ * PAINN_E_UNSUPPORTED (state_bits, grad_precision, more than 2^31 blocks of
+ * 4096 values), PAINN_E_OOM. */
+painn_status painn_adamw_create(painn_ctx* ctx, int32_t n_tensors, const painn_adamw_tensor* tensors,
+                                const painn_adamw_config* cfg, painn_adamw** out);
+/* One step at learning rate lr (finite, >= 0; else PAINN_E_ARG).  A captured
+ * step repeats with the lr and step number of its capture. */
+painn_status painn_adamw_step(painn_adamw* opt, double lr);
+/* Steps made so far (host). */
+painn_status painn_adamw_steps(const painn_adamw* opt, int64_t* steps);
+painn_status painn_adamw_free(painn_adamw* opt);
+
 /* ---- tracing ------------------------------------------------------------ */
 
 /* Per-kernel timing with HIP events on the context's stream (the build's

@@ -7,6 +7,7 @@ import os
 
 PAINN_FP64, PAINN_FP32, PAINN_BF16 = 0, 1, 2
 PRECISIONS = {"fp64": PAINN_FP64, "fp32": PAINN_FP32, "bf16": PAINN_BF16}
+ACTIVATIONS = {"none": 0, "silu": 1, "relu": 2, "gelu": 3}
 
 # every symbol declared in include/painn.h
 EXPORTS = [
@@ -17,12 +18,16 @@ EXPORTS = [
     "painn_forward_noalloc",
     "painn_forward_blend", "painn_forward_features", "painn_forces", "painn_forces_blend",
     "painn_trainer_create", "painn_trainer_step", "painn_trainer_params", "painn_trainer_free",
+    "painn_layer_norm", "painn_layer_norm_backward", "painn_linear", "painn_linear_backward",
+    "painn_grouped_linear", "painn_grouped_linear_backward",
+    "painn_adamw_create", "painn_adamw_step", "painn_adamw_steps", "painn_adamw_free",
     "painn_profile_enable",
     "painn_profile_read",
 ]
 
 _P = ctypes.c_void_p
 _I32 = ctypes.c_int32
+_I64 = ctypes.c_int64
 _SIGS = {
     "painn_create": ([ctypes.c_int, _P, ctypes.POINTER(_P)], ctypes.c_int),
     "painn_set_stream": ([_P, _P], ctypes.c_int),
@@ -52,6 +57,18 @@ _SIGS = {
     "painn_trainer_step": ([_P, _P, _P, _P, _P, _P], ctypes.c_int),
     "painn_trainer_params": ([_P, ctypes.POINTER(ctypes.c_int64), _P, _P], ctypes.c_int),
     "painn_trainer_free": ([_P], ctypes.c_int),
+    "painn_layer_norm": ([_P, ctypes.c_int, _I64, _I32, _P, _I64, _P, _P, ctypes.c_double, _P, _I64, _P, _P],
+                         ctypes.c_int),
+    "painn_layer_norm_backward": ([_P, ctypes.c_int, _I64, _I32, _P, _I64, _P, _I64, _P, _P, _P, _P, _I64, _P, _P],
+                                  ctypes.c_int),
+    "painn_linear": ([_P, _P], ctypes.c_int),
+    "painn_linear_backward": ([_P, _P], ctypes.c_int),
+    "painn_grouped_linear": ([_P, _P, _I32, _P], ctypes.c_int),
+    "painn_grouped_linear_backward": ([_P, _P, _I32, _P], ctypes.c_int),
+    "painn_adamw_create": ([_P, _I32, _P, _P, ctypes.POINTER(_P)], ctypes.c_int),
+    "painn_adamw_step": ([_P, ctypes.c_double], ctypes.c_int),
+    "painn_adamw_steps": ([_P, ctypes.POINTER(_I64)], ctypes.c_int),
+    "painn_adamw_free": ([_P], ctypes.c_int),
     "painn_profile_enable": ([_P, ctypes.c_int], ctypes.c_int),
     "painn_profile_read": ([_P, _I32, ctypes.POINTER(ctypes.c_char_p), ctypes.POINTER(ctypes.c_double),
                             ctypes.POINTER(ctypes.c_int64), ctypes.POINTER(_I32)], ctypes.c_int),
@@ -248,6 +265,88 @@ def painn_trainer_params(ctx: int, trainer: int, params: int | None = None, grad
 
 def painn_trainer_free(trainer: int) -> None:
     _check(load_library().painn_trainer_free(trainer))
+
+
+def painn_layer_norm(ctx: int, precision: int, rows: int, cols: int, x: int | None, ldx: int, gamma: int | None,
+                     beta: int | None, eps: float, y: int | None, ldy: int, mean: int | None,
+                     rstd: int | None) -> None:
+    _check(load_library().painn_layer_norm(ctx, precision, rows, cols, x, ldx, gamma, beta, eps, y, ldy, mean, rstd),
+           ctx)
+
+
+def painn_layer_norm_backward(ctx: int, precision: int, rows: int, cols: int, dy: int | None, lddy: int,
+                              x: int | None, ldx: int, gamma: int | None, mean: int | None, rstd: int | None,
+                              dx: int | None, lddx: int, dgamma: int | None, dbeta: int | None) -> None:
+    _check(load_library().painn_layer_norm_backward(ctx, precision, rows, cols, dy, lddy, x, ldx, gamma, mean, rstd,
+                                                    dx, lddx, dgamma, dbeta), ctx)
+
+
+class painn_linear_args(ctypes.Structure):
+    """include/painn.h painn_linear_args (host struct)."""
+    _fields_ = [("precision", _I32), ("activation", _I32), ("rows", _I64), ("d_in", _I32), ("d_out", _I32),
+                ("x", _P), ("ldx", _I64), ("w", _P), ("bias", _P), ("residual", _P), ("ldr", _I64),
+                ("y", _P), ("ldy", _I64), ("z", _P), ("ldz", _I64)]
+
+
+class painn_linear_backward_args(ctypes.Structure):
+    """include/painn.h painn_linear_backward_args (host struct)."""
+    _fields_ = [("precision", _I32), ("activation", _I32), ("rows", _I64), ("d_in", _I32), ("d_out", _I32),
+                ("dy", _P), ("lddy", _I64), ("z", _P), ("ldz", _I64), ("x", _P), ("ldx", _I64), ("w", _P),
+                ("xz", _P), ("ldxz", _I64), ("x_activation", _I32), ("reserved", _I32),
+                ("dx", _P), ("lddx", _I64), ("dw", _P), ("dbias", _P)]
+
+
+def painn_linear(ctx: int, args: painn_linear_args) -> None:
+    _check(load_library().painn_linear(ctx, ctypes.addressof(args)), ctx)
+
+
+def painn_linear_backward(ctx: int, args: painn_linear_backward_args) -> None:
+    _check(load_library().painn_linear_backward(ctx, ctypes.addressof(args)), ctx)
+
+
+def painn_grouped_linear(ctx: int, args: painn_linear_args, n_groups: int, offsets: int | None) -> None:
+    _check(load_library().painn_grouped_linear(ctx, ctypes.addressof(args), n_groups, offsets), ctx)
+
+
+def painn_grouped_linear_backward(ctx: int, args: painn_linear_backward_args, n_groups: int,
+                                  offsets: int | None) -> None:
+    _check(load_library().painn_grouped_linear_backward(ctx, ctypes.addressof(args), n_groups, offsets), ctx)
+
+
+class painn_adamw_tensor(ctypes.Structure):
+    """include/painn.h painn_adamw_tensor (host struct)."""
+    _fields_ = [("n", _I64), ("param", _P), ("grad", _P), ("copy", _P), ("m", _P), ("v", _P), ("m_scale", _P),
+                ("v_scale", _P)]
+
+
+class painn_adamw_config(ctypes.Structure):
+    """include/painn.h painn_adamw_config (host struct)."""
+    _fields_ = [("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("weight_decay", ctypes.c_double), ("state_bits", _I32), ("grad_precision", _I32), ("steps", _I64)]
+
+
+def painn_adamw_create(ctx: int, tensors: list, cfg: dict) -> int:
+    """tensors: dicts of painn_adamw_tensor's fields (absent: null)."""
+    out = _P()
+    t = (painn_adamw_tensor * max(1, len(tensors)))(*[painn_adamw_tensor(**x) for x in tensors])
+    c = painn_adamw_config(**cfg)
+    _check(load_library().painn_adamw_create(ctx, len(tensors), ctypes.addressof(t), ctypes.addressof(c),
+                                             ctypes.byref(out)), ctx)
+    return out.value
+
+
+def painn_adamw_step(ctx: int, opt: int, lr: float) -> None:
+    _check(load_library().painn_adamw_step(opt, lr), ctx)
+
+
+def painn_adamw_steps(opt: int) -> int:
+    n = _I64()
+    _check(load_library().painn_adamw_steps(opt, ctypes.byref(n)))
+    return n.value
+
+
+def painn_adamw_free(opt: int) -> None:
+    _check(load_library().painn_adamw_free(opt))
 
 
 def painn_profile_enable(ctx: int, enable: bool) -> None:

@@ -1,0 +1,684 @@
+// Dense layers with bias, activation and residual in the epilogue, one weight
+// matrix for all rows or one per group of consecutive rows, and their reverse
+// pass (FP32, BF16).
+//
+// All three products are one tile kernel, D[m][n] = sum_k A[m][k] B[n][k]:
+//   forward  A = x, B = w;   dx  A = dz, B = w^T;   dw  A = dz^T, B = x^T.
+// A block stages BK values of k of both operands in LDS as [row][k] in BF16 (a
+// transposed operand is turned on the way), its waves feed 16x16x32 matrix
+// instructions from there, and the next k-block's loads are in flight
+// meanwhile.  The weights are the instruction's first operand, so that a lane
+// ends up with four neighbouring columns of one row.
+//
+// FP32 operands become three BF16 planes on the way into LDS (split3, mfma.h)
+// and six of the nine plane products are formed: 96 matrix-core cycles per
+// 16x16x32 against 256 of the FP32 instruction, at FP32's accuracy.
+//
+// Rows of a ragged batch are tiled per group: a block finds its tile by a scan
+// over the groups' row counts, one group per lane, so that no launch or
+// readback plans the tiles.  dw contracts over the rows: each group's rows are
+// cut into chunks of a fixed length, one block per chunk and tile of dw, and
+// where a group has several chunks k_fold adds their FP32 parts in order.
+#include "mfma.h"
+#include "ops.h"
+
+namespace {
+
+using namespace ops;
+
+typedef uint32_t u4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u2_t __attribute__((ext_vector_type(2)));
+
+// ---- groups ---------------------------------------------------------------------
+struct Groups {
+  int n;                        // 0: one group of all rows
+  const int32_t* offsets;
+  long long rows;
+};
+struct Span {
+  int g;                        // group, -1: none
+  int index;                    // tile within the group
+  int count;                    // tiles of the group
+  long long lo, hi;             // rows of the group
+};
+
+// Rows [lo, hi) of group g, within [0, rows] whatever the offsets are.
+__device__ __forceinline__ void group_rows(const Groups& gr, int g, long long& lo, long long& hi) {
+  lo = gr.offsets[g];
+  hi = gr.offsets[g + 1];
+  lo = lo < 0 ? 0 : lo > gr.rows ? gr.rows : lo;
+  hi = hi < lo ? lo : hi > gr.rows ? gr.rows : hi;
+}
+
+// Tile t of all groups' tiles of `len` rows, at least `least` per group.  Every
+// wave of the block finds the same.
+__device__ __forceinline__ Span find_tile(const Groups& gr, int t, int len, int least) {
+  Span s{-1, 0, 0, 0, 0};
+  if (gr.n == 0) {
+    const int tiles = (int)((gr.rows + len - 1) / len);
+    s.count = tiles < least ? least : tiles;
+    if (t < s.count) {
+      s.g = 0;
+      s.index = t;
+      s.hi = gr.rows;
+    }
+    return s;
+  }
+  const int lane = threadIdx.x & 63;
+  int before = 0;
+  for (int g0 = 0; g0 < gr.n; g0 += 64) {
+    long long lo = 0, hi = 0;
+    int tiles = 0;
+    if (g0 + lane < gr.n) {
+      group_rows(gr, g0 + lane, lo, hi);
+      tiles = (int)((hi - lo + len - 1) / len);
+      tiles = tiles < least ? least : tiles;
+    }
+    int end = tiles;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int x = __shfl_up(end, o);
+      if (lane >= o) end += x;
+    }
+    end += before;
+    const unsigned long long past = __ballot(t < end);
+    if (past) {
+      const int l = __ffsll((long long)past) - 1;
+      s.g = g0 + l;
+      s.count = __shfl(tiles, l);
+      s.index = t - (__shfl(end, l) - s.count);
+      s.lo = __shfl((int)lo, l);
+      s.hi = __shfl((int)hi, l);
+      // (offsets that decrease may count more tiles than there are)
+      if (s.index < 0 || s.index >= s.count) s.g = -1;
+      return s;
+    }
+    before = __shfl(end, 63);
+  }
+  return s;
+}
+
+// ---- operands -------------------------------------------------------------------
+template <class T> struct Mma;
+template <> struct Mma<b16> {
+  static constexpr int NP = 1, NSUB = 1, BK = 64;
+};
+template <> struct Mma<float> {
+  static constexpr int NP = 3, NSUB = 6, BK = 32;
+};
+
+// An LDS tile is [row][BK] per plane, its 16-byte chunks permuted within the
+// row so that the 16 rows of a fragment, and the rows a transposing store
+// writes together, fall into different banks.
+template <int BK>
+__device__ __forceinline__ int lds_at(int row, int c) {
+  const int s = BK == 64 ? (row ^ (row >> 3)) & 7 : ((row >> 1) ^ (row >> 3)) & 3;
+  return row * BK + ((c ^ s) << 3);
+}
+
+// What one thread carries of a k-block of an operand: R rows x BK.
+// Plain: the operand is [row][k]; units of 8 k.
+// TR: it is [k][row]; units of 4 k x 8 rows (BF16) or 4 k x 4 rows (FP32).
+template <class T, int R, int TH, bool TR>
+struct Stage {
+  static constexpr int BK = Mma<T>::BK, CH = BK / 8;
+  static constexpr bool B = sizeof(T) == 2;
+  static constexpr int RU = B ? 8 : 4;                                 // rows of a transposed unit
+  static constexpr int UNITS = TR ? R * BK / (4 * RU) : R * BK / 8;
+  static constexpr int U = (UNITS + TH - 1) / TH;
+  static constexpr int W = B && !TR ? 1 : B ? 4 : TR ? 4 : 2;          // 16-byte words of a unit
+  u4_t w[U][W];
+
+  __device__ __forceinline__ static u4_t word(const T* p) {
+    u4_t v;
+    __builtin_memcpy(&v, p, 16);
+    return v;
+  }
+  // the first n elements of a 16-byte word
+  __device__ __forceinline__ static u4_t word_n(const T* p, long long n) {
+    constexpr int E = 16 / sizeof(T);
+    u4_t v = {0, 0, 0, 0};
+    if (n >= E) return word(p);
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (e < n) {
+        if constexpr (B) {
+          uint16_t h;
+          __builtin_memcpy(&h, p + e, 2);
+          v[e / 2] |= (uint32_t)h << (16 * (e & 1));
+        } else {
+          uint32_t x;
+          __builtin_memcpy(&x, p + e, 4);
+          v[e] = x;
+        }
+      }
+    return v;
+  }
+
+  // k-block [k0, k0 + BK) of rows [r0, r0 + R); rows < n_rows, k < n_k exist
+  // (n_rows, n_k >= 1).  What lies past n_k is zero; rows past n_rows hold
+  // anything.
+  __device__ __forceinline__ void load(const T* base, long long ld, long long r0, long long n_rows, long long k0,
+                                       long long n_k) {
+    const int tid = threadIdx.x;
+    const bool full = k0 + BK <= n_k && (!TR || r0 + R <= n_rows);
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int u = i * TH + tid;
+      if (UNITS % TH != 0 && u >= UNITS) break;
+      if constexpr (!TR) {
+        long long r = r0 + u / CH;
+        r = r < n_rows ? r : n_rows - 1;
+        const long long k = k0 + (u % CH) * 8;
+        const T* p = base + r * ld + k;
+        if (full) {
+#pragma unroll
+          for (int j = 0; j < W; ++j) w[i][j] = word(p + j * (16 / sizeof(T)));
+        } else {
+#pragma unroll
+          for (int j = 0; j < W; ++j) w[i][j] = word_n(p + j * (16 / sizeof(T)), n_k - k - j * (int)(16 / sizeof(T)));
+        }
+      } else {
+        const long long r = r0 + (u % (R / RU)) * RU;
+        const long long k = k0 + (u / (R / RU)) * 4;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const T* p = base + (k + j) * ld + r;
+          if (full) w[i][j] = word(p);
+          else w[i][j] = k + j < n_k ? word_n(p, n_rows - r) : u4_t{0, 0, 0, 0};
+        }
+      }
+    }
+  }
+
+  // Four k of one row and the planes of their values.
+  __device__ __forceinline__ static void put4(uint16_t* lds, int at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    uint32_t p[4][3];
+    split3(__uint_as_float(a), p[0]);
+    split3(__uint_as_float(b), p[1]);
+    split3(__uint_as_float(c), p[2]);
+    split3(__uint_as_float(d), p[3]);
+#pragma unroll
+    for (int q = 0; q < 3; ++q)
+      *(u2_t*)(lds + (size_t)q * R * BK + at) = u2_t{(p[0][q] >> 16) | p[1][q], (p[2][q] >> 16) | p[3][q]};
+  }
+
+  __device__ __forceinline__ void put(uint16_t* lds) const {
+    const int tid = threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int u = i * TH + tid;
+      if (UNITS % TH != 0 && u >= UNITS) break;
+      if constexpr (!TR) {
+        const int at = lds_at<BK>(u / CH, u % CH);
+        if constexpr (B) {
+          *(u4_t*)(lds + at) = w[i][0];
+        } else {
+          put4(lds, at, w[i][0][0], w[i][0][1], w[i][0][2], w[i][0][3]);
+          put4(lds, at + 4, w[i][1][0], w[i][1][1], w[i][1][2], w[i][1][3]);
+        }
+      } else {
+        const int r = (u % (R / RU)) * RU, kg = u / (R / RU);
+#pragma unroll
+        for (int e = 0; e < RU; ++e) {
+          const int at = lds_at<BK>(r + e, kg >> 1) + 4 * (kg & 1);
+          if constexpr (B) {
+            uint32_t x[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = w[i][j][e >> 1];
+            const uint32_t sel = e & 1 ? 0x07060302u : 0x05040100u;     // the upper or lower halves of a pair
+            *(u2_t*)(lds + at) = u2_t{__builtin_amdgcn_perm(x[1], x[0], sel), __builtin_amdgcn_perm(x[3], x[2], sel)};
+          } else {
+            put4(lds, at, w[i][0][e], w[i][1][e], w[i][2][e], w[i][3][e]);
+          }
+        }
+      }
+    }
+  }
+};
+
+// ---- the tile kernel --------------------------------------------------------------
+enum { FWD = 0, DX = 1, DW = 2 };
+
+struct Args {
+  Groups gr;
+  int d_in, d_out;
+  const void* a;  long long lda;     // x (FWD), dz (DX, DW)
+  const void* b;  long long ldb;     // w [g][d_out][d_in] (FWD, DX), x (DW)
+  const void* bias;
+  int act;                           // FWD: of z; DX: of xz
+  const void* e;  long long lde;     // FWD: residual, DX: xz
+  void* out;      long long ldo;     // y, dx, dw
+  void* z;        long long ldz;     // FWD
+  void* db;                          // DW
+  float* part;                       // DW: [slot][d_out][d_in] of groups with several chunks
+  float* part_b;                     // DW: [slot][d_out]
+  int chunk;                         // DW: rows of a chunk
+  int tiles;                         // FWD, DX: row tiles (an upper bound); DW: chunks
+  int nt;                            // column tiles of a row tile; DW: tiles of dw
+  int nt_in;                         // DW: tiles along d_in
+};
+
+template <class T, int BM, int BN, int WM, int WN, int MODE>
+__global__ void __launch_bounds__(64 * WM * WN, 2) k_dense(Args g) {
+  using M = Mma<T>;
+  constexpr int NP = M::NP, BK = M::BK, TH = 64 * WM * WN;
+  constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
+  __shared__ __attribute__((aligned(16))) uint16_t As[NP * BM * BK], Bs[NP * BN * BK];
+  // Many row tiles: the column tiles of one on one XCD, next to each other, so
+  // that its rows are read from that L2.  Few: all tiles over all XCDs.
+  const bool many = g.tiles >= 64;
+  const int lin = many ? blockIdx.x >> 3 : blockIdx.x;
+  const int t = many ? (lin / g.nt) * 8 + (blockIdx.x & 7) : lin / g.nt, c = lin % g.nt;
+  if (t >= g.tiles) return;
+  const Span s = find_tile(g.gr, t, MODE == DW ? g.chunk : BM, MODE == DW ? 1 : 0);
+  if (s.g < 0) return;
+
+  const T *a = (const T*)g.a, *b = (const T*)g.b;
+  const size_t wsize = (size_t)g.d_out * g.d_in;
+  long long m0, m_end, n0, n_end, nk;
+  if constexpr (MODE == DW) {
+    const long long lo = s.lo + (long long)s.index * g.chunk;
+    nk = s.hi - lo < g.chunk ? s.hi - lo : g.chunk;
+    a += lo * g.lda;
+    b += lo * g.ldb;
+    m0 = (long long)(c / g.nt_in) * BM;
+    n0 = (long long)(c % g.nt_in) * BN;
+    m_end = g.d_out;
+    n_end = g.d_in;
+  } else {
+    m0 = s.lo + (long long)s.index * BM;
+    m_end = s.hi;
+    n0 = (long long)c * BN;
+    n_end = MODE == FWD ? g.d_out : g.d_in;
+    nk = MODE == FWD ? g.d_in : g.d_out;
+    b += (size_t)s.g * wsize;
+  }
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, lr = lane & 15, lq = lane >> 4;
+  const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
+  const bool sum_b = MODE == DW && g.db != nullptr && n0 == 0 && wn == 0;
+
+  f4_t acc[FM][FN], accb[MODE == DW ? FM : 1];
+#pragma unroll
+  for (int i = 0; i < FM; ++i) {
+    if constexpr (MODE == DW) accb[i] = f4_t{0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < FN; ++j) acc[i][j] = f4_t{0, 0, 0, 0};
+  }
+  bf8_t ones;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) ones[i] = (b16)1.f;
+
+  Stage<T, BM, TH, MODE == DW> sa;
+  Stage<T, BN, TH, MODE != FWD> sb;
+  if (nk > 0) {
+    sa.load(a, g.lda, m0, m_end, 0, nk);
+    sb.load(b, g.ldb, n0, n_end, 0, nk);
+  }
+  for (long long k0 = 0; k0 < nk; k0 += BK) {
+    sa.put(As);
+    sb.put(Bs);
+    __syncthreads();
+    if (k0 + BK < nk) {
+      sa.load(a, g.lda, m0, m_end, k0 + BK, nk);
+      sb.load(b, g.ldb, n0, n_end, k0 + BK, nk);
+    }
+#pragma unroll
+    for (int kk = 0; kk < BK / 32; ++kk) {
+      bf8_t fa[FM][NP], fb[FN][NP];
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int p = 0; p < NP; ++p)
+          fa[i][p] = *(const bf8_t*)(As + p * BM * BK + lds_at<BK>(wm + 16 * i + lr, 4 * kk + lq));
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+#pragma unroll
+        for (int p = 0; p < NP; ++p)
+          fb[j][p] = *(const bf8_t*)(Bs + p * BN * BK + lds_at<BK>(wn + 16 * j + lr, 4 * kk + lq));
+      // smallest products first: lo hi, mid mid, hi lo, mid hi, hi mid, hi hi
+      constexpr int pa[6] = {2, 1, 0, 1, 0, 0}, pb[6] = {0, 1, 2, 0, 1, 0};
+#pragma unroll
+      for (int q = 0; q < M::NSUB; ++q) {
+        const int qa = NP == 1 ? 0 : pa[q], qb = NP == 1 ? 0 : pb[q];
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+          for (int j = 0; j < FN; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j][qb], fa[i][qa], acc[i][j], 0, 0, 0);
+      }
+      if constexpr (MODE == DW)
+        if (sum_b) {
+          // the column sums of dz, as a product with ones
+#pragma unroll
+          for (int p = NP - 1; p >= 0; --p)
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+              accb[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, fa[i][p], accb[i], 0, 0, 0);
+        }
+    }
+    __syncthreads();
+  }
+
+  if constexpr (MODE == DW) {
+    const bool whole = s.count == 1;
+    float* part = whole ? nullptr : g.part + (size_t)t * wsize;
+    T* out = (T*)g.out + (size_t)s.g * wsize;
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+      const long long m = m0 + wm + 16 * i + lr;
+      if (m >= m_end) continue;
+#pragma unroll
+      for (int j = 0; j < FN; ++j) {
+        const long long n = n0 + wn + 16 * j + 4 * lq;
+        if (n >= n_end) continue;
+        float v[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = acc[i][j][r];
+        if (whole) store_n<4>(out + m * g.d_in + n, n_end - n, v);
+        else store_n<4>(part + m * g.d_in + n, n_end - n, v);
+      }
+      if (sum_b && lq == 0) {
+        const float v = accb[i][0];
+        if (whole) store<1>((T*)g.db + (size_t)s.g * g.d_out + m, &v);
+        else g.part_b[(size_t)t * g.d_out + m] = v;
+      }
+    }
+  } else {
+    float bias[FN][4];
+    if constexpr (MODE == FWD) {
+#pragma unroll
+      for (int j = 0; j < FN; ++j) {
+        const long long n = n0 + wn + 16 * j + 4 * lq;
+        if (g.bias) load_n<4>((const T*)g.bias + (size_t)s.g * g.d_out + n, n_end - n, bias[j]);
+        else bias[j][0] = bias[j][1] = bias[j][2] = bias[j][3] = 0.f;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+      const long long m = m0 + wm + 16 * i + lr;
+      if (m >= m_end) continue;
+#pragma unroll
+      for (int j = 0; j < FN; ++j) {
+        const long long n = n0 + wn + 16 * j + 4 * lq, left = n_end - n;
+        if (left <= 0) continue;
+        float v[4], e[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = acc[i][j][r];
+        if constexpr (MODE == FWD) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) v[r] += bias[j][r];
+          if (g.z) store_n<4>((T*)g.z + m * g.ldz + n, left, v);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) v[r] = act(v[r], g.act);
+          if (g.e) {
+            load_n<4>((const T*)g.e + m * g.lde + n, left, e);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) v[r] += e[r];
+          }
+        } else if (g.act != PAINN_ACT_NONE) {
+          load_n<4>((const T*)g.e + m * g.lde + n, left, e);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) v[r] *= act_slope(e[r], g.act);
+        }
+        store_n<4>((T*)g.out + m * g.ldo + n, left, v);
+      }
+    }
+  }
+}
+
+// dz = dy activation'(z), [rows][d_out] without gaps.
+template <class T>
+__global__ void __launch_bounds__(256) k_dz(long long rows, int d_out, const T* __restrict__ dy, long long lddy,
+                                            const T* __restrict__ z, long long ldz, int kind, T* __restrict__ dz) {
+  constexpr int V = 16 / sizeof(T);
+  const int per = (d_out + V - 1) / V;
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (i >= rows * per) return;
+  const long long r = i / per;
+  const int c = (int)(i - r * per) * V;
+  float d[V], s[V];
+  load_n<V>(dy + r * lddy + c, d_out - c, d);
+  load_n<V>(z + r * ldz + c, d_out - c, s);
+#pragma unroll
+  for (int k = 0; k < V; ++k) d[k] *= act_slope(s[k], kind);
+  store_n<V>(dz + r * d_out + c, d_out - c, d);
+}
+
+// dw and dbias of the groups that have several chunks: their parts added in
+// the order of the rows.  blockIdx.y: the group.
+template <class T>
+__global__ void __launch_bounds__(256) k_fold(Args g) {
+  const int grp = blockIdx.y, lane = threadIdx.x & 63;
+  // the group's first chunk, by the same count as find_tile's
+  int first = 0, count = 0;
+  if (g.gr.n == 0) {
+    count = (int)((g.gr.rows + g.chunk - 1) / g.chunk);
+  } else {
+    long long lo, hi;
+    for (int k = lane; k < grp; k += 64) {
+      group_rows(g.gr, k, lo, hi);
+      const int n = (int)((hi - lo + g.chunk - 1) / g.chunk);
+      first += n < 1 ? 1 : n;
+    }
+#pragma unroll
+    for (int o = 32; o; o >>= 1) first += __shfl_xor(first, o);
+    group_rows(g.gr, grp, lo, hi);
+    count = (int)((hi - lo + g.chunk - 1) / g.chunk);
+  }
+  if (count > g.tiles - first) count = g.tiles - first;   // (offsets that decrease)
+  if (first < 0 || count <= 1) return;
+  const size_t wsize = (size_t)g.d_out * g.d_in;
+  const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (i < wsize) {
+    const float* p = g.part + (size_t)first * wsize + i;
+    float sum[4] = {0, 0, 0, 0}, v[4];
+    for (int k = 0; k < count; ++k, p += wsize) {
+      load_n<4>(p, (long long)(wsize - i), v);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] += v[e];
+    }
+    store_n<4>((T*)g.out + (size_t)grp * wsize + i, (long long)(wsize - i), sum);
+  }
+  if (g.db)
+    for (size_t o = (size_t)blockIdx.x * 256 + threadIdx.x; o < (size_t)g.d_out; o += (size_t)gridDim.x * 256) {
+      float sum = 0.f;
+      for (int k = 0; k < count; ++k) sum += g.part_b[(size_t)(first + k) * g.d_out + o];
+      store<1>((T*)g.db + (size_t)grp * g.d_out + o, &sum);
+    }
+}
+
+inline long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
+
+// Upper bound of the row tiles of `len` rows.
+inline long long tile_bound(const Groups& gr, int len, int least) {
+  const long long n = ceil_div(gr.rows, len);
+  return gr.n ? n + gr.n : n < least ? least : n;
+}
+
+template <class T, int BM, int BN, int WM, int WN, int MODE>
+bool launch(hipStream_t st, Args a, long long tiles, long long nt) {
+  if (tiles > 0x7fffffffLL / (nt < 8 ? 8 : nt) - 8) return false;
+  const long long blocks = (tiles >= 64 ? ceil_div(tiles, 8) * 8 : tiles) * nt;
+  if (blocks == 0) return true;
+  a.tiles = (int)tiles;
+  a.nt = (int)nt;
+  k_dense<T, BM, BN, WM, WN, MODE><<<dim3((unsigned)blocks), 64 * WM * WN, 0, st>>>(a);
+  return true;
+}
+
+// Blocks that fill the card: 256 CUs, two blocks each.
+constexpr long long FULL = 512;
+
+// FWD and DX: tiles of 128 x 128, or of 64 x 64 where those leave CUs idle.
+template <class T, int MODE>
+bool run_rows(hipStream_t st, const Args& a) {
+  const int width = MODE == FWD ? a.d_out : a.d_in;
+  const long long big = tile_bound(a.gr, 128, 0) * ceil_div(width, 128);
+  if (big >= FULL / 2)
+    return launch<T, 128, 128, 2, 2, MODE>(st, a, tile_bound(a.gr, 128, 0), ceil_div(width, 128));
+  return launch<T, 64, 64, 2, 2, MODE>(st, a, tile_bound(a.gr, 64, 0), ceil_div(width, 64));
+}
+
+template <class T>
+painn_status run_fwd(painn_ctx* ctx, const painn_linear_args& p, int n_groups, const int32_t* offsets) {
+  Args a{};
+  a.gr = Groups{n_groups, offsets, p.rows};
+  a.d_in = p.d_in; a.d_out = p.d_out;
+  a.a = p.x; a.lda = p.ldx;
+  a.b = p.w; a.ldb = p.d_in;
+  a.bias = p.bias;
+  a.act = p.activation;
+  a.e = p.residual; a.lde = p.ldr;
+  a.out = p.y; a.ldo = p.ldy;
+  a.z = p.z; a.ldz = p.ldz;
+  prof_mark(ctx->prof, ctx->stream, KC_LINEAR, true);
+  const bool ok = run_rows<T, FWD>(ctx->stream, a);
+  prof_mark(ctx->prof, ctx->stream, KC_LINEAR, false);
+  if (!ok) return fail(ctx, PAINN_E_UNSUPPORTED, "more than 2^31 tiles");
+  return launched(ctx, "dense layer launch");
+}
+
+template <class T>
+painn_status run_bwd(painn_ctx* ctx, const painn_linear_backward_args& p, int n_groups, const int32_t* offsets) {
+  const int G = n_groups ? n_groups : 1;
+  Args a{};
+  a.gr = Groups{n_groups, offsets, p.rows};
+  a.d_in = p.d_in; a.d_out = p.d_out;
+  a.a = p.dy; a.lda = p.lddy;
+  // dw: chunks of rows so that its tiles fill the card
+  const size_t wsize = (size_t)p.d_out * p.d_in;
+  const bool big = p.d_in > 64 && p.d_out > 64;
+  const int bt = big ? 128 : 64;
+  const long long nt = ceil_div(p.d_out, bt) * ceil_div(p.d_in, bt);
+  const long long want = ceil_div(FULL, nt);
+  const long long chunk = ((ceil_div(p.rows, want) + 255) / 256) * 256;
+  a.chunk = (int)(chunk < 256 ? 256 : chunk > (1 << 24) ? 1 << 24 : chunk);
+  const long long slots = tile_bound(a.gr, a.chunk, 1);
+  const bool have_dz = p.activation != PAINN_ACT_NONE && p.rows > 0;
+  const size_t dz_bytes = have_dz ? align256((size_t)p.rows * p.d_out * sizeof(T)) : 0;
+  // (one chunk per group: no parts)
+  const bool parts = p.dw && ceil_div(p.rows, a.chunk) > 1;
+  const size_t part_bytes = parts ? align256((size_t)slots * wsize * sizeof(float)) : 0;
+  const size_t need = dz_bytes + part_bytes + (parts ? (size_t)slots * p.d_out * sizeof(float) : 0);
+  if (need) {
+    const painn_status st = ops_workspace(ctx, need);
+    if (st != PAINN_OK) return st;
+  }
+  char* ws = (char*)ctx->bws.p;
+  const hipStream_t st = ctx->stream;
+  prof_mark(ctx->prof, st, KC_LINEAR_BWD, true);
+  bool ok = true;
+  if (have_dz) {
+    const long long blocks = ceil_div(p.rows * ceil_div(p.d_out, 16 / sizeof(T)), 256);
+    ok = blocks <= 0x7fffffffLL;
+    if (ok)
+      k_dz<T><<<dim3((unsigned)blocks), 256, 0, st>>>(p.rows, p.d_out, (const T*)p.dy, p.lddy, (const T*)p.z, p.ldz,
+                                                     p.activation, (T*)ws);
+    a.a = ws;
+    a.lda = p.d_out;
+  }
+  if (ok && p.dw) {
+    Args d = a;
+    d.b = p.x; d.ldb = p.ldx;
+    d.out = p.dw;
+    d.db = p.dbias;
+    d.part = (float*)(ws + dz_bytes);
+    d.part_b = (float*)(ws + dz_bytes + part_bytes);
+    d.nt_in = (int)ceil_div(p.d_in, bt);
+    d.tiles = (int)slots;
+    ok = big ? launch<T, 128, 128, 2, 2, DW>(st, d, slots, nt) : launch<T, 64, 64, 2, 2, DW>(st, d, slots, nt);
+    if (ok && parts) k_fold<T><<<dim3((unsigned)ceil_div(wsize, 1024), G), 256, 0, st>>>(d);
+  }
+  if (ok && p.dx && p.rows > 0) {
+    Args d = a;
+    d.b = p.w; d.ldb = p.d_in;
+    d.act = p.x_activation;
+    d.e = p.xz; d.lde = p.ldxz;
+    d.out = p.dx; d.ldo = p.lddx;
+    ok = run_rows<T, DX>(st, d);
+  }
+  prof_mark(ctx->prof, st, KC_LINEAR_BWD, false);
+  if (!ok) return fail(ctx, PAINN_E_UNSUPPORTED, "more than 2^31 tiles");
+  return launched(ctx, "dense layer reverse launch");
+}
+
+bool known_act(int a) { return a >= PAINN_ACT_NONE && a <= PAINN_ACT_GELU; }
+
+painn_status dense_check(painn_ctx* ctx, int prec, int act, int x_act, int64_t rows, int d_in, int d_out,
+                         int n_groups, const int32_t* offsets, bool grouped) {
+  if (prec == PAINN_FP64) return fail(ctx, PAINN_E_UNSUPPORTED, "the dense layer runs in FP32 and BF16");
+  if (prec != PAINN_FP32 && prec != PAINN_BF16) return fail(ctx, PAINN_E_ARG, "unknown precision");
+  if (!known_act(act) || !known_act(x_act)) return fail(ctx, PAINN_E_ARG, "unknown activation");
+  if (d_in < 1 || d_out < 1) return fail(ctx, PAINN_E_ARG, "widths must be at least 1");
+  if (rows < 0) return fail(ctx, PAINN_E_ARG, "rows must not be negative");
+  if (d_in > (1 << 20) || d_out > (1 << 20)) return fail(ctx, PAINN_E_UNSUPPORTED, "widths above 2^20");
+  if (grouped) {
+    if (n_groups < 1 || n_groups > 4096) return fail(ctx, PAINN_E_ARG, "n_groups must be in [1, 4096]");
+    if (!offsets) return fail(ctx, PAINN_E_ARG, "null offsets");
+    if (rows > 0x7fffffffLL) return fail(ctx, PAINN_E_ARG, "grouped rows must be below 2^31");
+  }
+  return PAINN_OK;
+}
+
+painn_status fwd_entry(painn_ctx* ctx, const painn_linear_args* p, int n_groups, const int32_t* offsets, bool grouped) {
+  if (!ctx) return PAINN_E_ARG;
+  ctx->err.clear();
+  if (!p) return fail(ctx, PAINN_E_ARG, "null args");
+  const painn_status st = dense_check(ctx, p->precision, p->activation, 0, p->rows, p->d_in, p->d_out, n_groups,
+                                      offsets, grouped);
+  if (st != PAINN_OK) return st;
+  if (p->rows == 0) return PAINN_OK;
+  if (!p->x || !p->w || !p->y) return fail(ctx, PAINN_E_ARG, "null array");
+  if (p->ldx < p->d_in || p->ldy < p->d_out || (p->residual && p->ldr < p->d_out) || (p->z && p->ldz < p->d_out))
+    return fail(ctx, PAINN_E_ARG, "a row stride is below the row's width");
+  (void)hipSetDevice(ctx->device);
+  (void)hipGetLastError();
+  return p->precision == PAINN_FP32 ? run_fwd<float>(ctx, *p, n_groups, offsets)
+                                    : run_fwd<b16>(ctx, *p, n_groups, offsets);
+}
+
+painn_status bwd_entry(painn_ctx* ctx, const painn_linear_backward_args* p, int n_groups, const int32_t* offsets,
+                       bool grouped) {
+  if (!ctx) return PAINN_E_ARG;
+  ctx->err.clear();
+  if (!p) return fail(ctx, PAINN_E_ARG, "null args");
+  const painn_status st = dense_check(ctx, p->precision, p->activation, p->x_activation, p->rows, p->d_in, p->d_out,
+                                      n_groups, offsets, grouped);
+  if (st != PAINN_OK) return st;
+  if (p->dbias && !p->dw) return fail(ctx, PAINN_E_ARG, "dbias is formed with dw");
+  if (p->rows > 0) {
+    if (!p->dy || (p->activation != PAINN_ACT_NONE && !p->z) || (p->dw && !p->x) || (p->dx && !p->w) ||
+        (p->dx && p->x_activation != PAINN_ACT_NONE && !p->xz))
+      return fail(ctx, PAINN_E_ARG, "null array");
+    if (p->lddy < p->d_out || (p->activation != PAINN_ACT_NONE && p->ldz < p->d_out) || (p->dw && p->ldx < p->d_in) ||
+        (p->dx && p->lddx < p->d_in) || (p->dx && p->x_activation != PAINN_ACT_NONE && p->ldxz < p->d_in))
+      return fail(ctx, PAINN_E_ARG, "a row stride is below the row's width");
+  }
+  if (!p->dw && (!p->dx || p->rows == 0)) return PAINN_OK;
+  (void)hipSetDevice(ctx->device);
+  (void)hipGetLastError();
+  return p->precision == PAINN_FP32 ? run_bwd<float>(ctx, *p, n_groups, offsets)
+                                    : run_bwd<b16>(ctx, *p, n_groups, offsets);
+}
+
+}  // namespace
+
+extern "C" {
+
+painn_status painn_linear(painn_ctx* ctx, const painn_linear_args* args) {
+  return fwd_entry(ctx, args, 0, nullptr, false);
+}
+painn_status painn_linear_backward(painn_ctx* ctx, const painn_linear_backward_args* args) {
+  return bwd_entry(ctx, args, 0, nullptr, false);
+}
+painn_status painn_grouped_linear(painn_ctx* ctx, const painn_linear_args* args, int32_t n_groups,
+                                  const int32_t* offsets) {
+  return fwd_entry(ctx, args, n_groups, offsets, true);
+}
+painn_status painn_grouped_linear_backward(painn_ctx* ctx, const painn_linear_backward_args* args, int32_t n_groups,
+                                           const int32_t* offsets) {
+  return bwd_entry(ctx, args, n_groups, offsets, true);
+}
+
+}  // extern "C"

@@ -10,6 +10,7 @@
 
 #include "branchgemm.h"
 #include "internal.h"
+#include "ops.h"
 
 namespace {
 
@@ -448,17 +449,17 @@ struct Profiler {
   std::vector<hipEvent_t> pool;
   struct Rec { int kc; hipEvent_t a, b; };
   std::vector<Rec> recs;
-  hipEvent_t open[KC_COUNT] = {};
-  double ms[KC_COUNT] = {};
-  long long launches[KC_COUNT] = {};
+  hipEvent_t open[KC_ALL] = {};
+  double ms[KC_ALL] = {};
+  long long launches[KC_ALL] = {};
 };
 
 static const char* kc_name(int kc) {
-  static const char* names[KC_COUNT] = {"graph_prep", "graph_count", "graph_scan", "graph_fill",
+  static const char* names[KC_ALL] = {"graph_prep", "graph_count", "graph_scan", "graph_fill",
                                         "embed", "phi", "edge_prep", "message", "update", "heads",
                                         "energy", "export", "transpose", "bwd_heads", "bwd_update",
                                         "bwd_message", "bwd_phi", "force", "train_real", "train_tangent",
-                                        "train_adamw"};
+                                        "train_adamw", "norm", "bwd_norm", "linear", "bwd_linear", "adamw"};
   return names[kc];
 }
 
@@ -1282,17 +1283,26 @@ painn_status painn_profile_read(painn_ctx* ctx, int32_t n_max, const char** name
   HIP_TRY(ctx, hipStreamSynchronize(ctx->stream));
   prof_collect(ctx->prof);
   int n = 0;
-  for (int k = 0; k < KC_COUNT && n < n_max; ++k) {
+  for (int k = 0; k < KC_ALL && n < n_max; ++k) {
     if (!ctx->prof->launches[k]) continue;
     names[n] = kc_name(k);
     ms[n] = ctx->prof->ms[k];
     launches[n] = ctx->prof->launches[k];
     ++n;
   }
-  for (int k = 0; k < KC_COUNT; ++k) { ctx->prof->ms[k] = 0; ctx->prof->launches[k] = 0; }
+  for (int k = 0; k < KC_ALL; ++k) { ctx->prof->ms[k] = 0; ctx->prof->launches[k] = 0; }
   *n_out = n;
   return PAINN_OK;
 }
 
 }  // extern "C"
 
+painn_status ops_workspace(painn_ctx* ctx, size_t need) {
+  if (need <= ctx->bws.bytes) return PAINN_OK;
+  if (capturing(ctx))
+    return fail(ctx, PAINN_E_OOM, "the workspace of " + std::to_string(need) +
+                                      " bytes is not there and cannot be allocated while the stream is captured");
+  if (!grow_workspace(ctx, ctx->bws, need, need, 8))
+    return fail(ctx, PAINN_E_OOM, "workspace allocation of " + std::to_string(need) + " bytes failed");
+  return PAINN_OK;
+}

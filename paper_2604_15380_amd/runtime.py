@@ -3,6 +3,7 @@ stream come from torch; every computation runs in libpainn.so."""
 from __future__ import annotations
 
 import ctypes
+import sys
 
 import numpy as np
 
@@ -67,6 +68,106 @@ class Graph:
         if self.handle:
             B.painn_graph_free(self.handle)
             self.handle = 0
+
+
+class AdamW:
+    """AdamW over many tensors, one launch per step (painn_adamw_*).
+
+    The optimizer reads `grads` and writes `params` (and `copies`) in place.
+    state_bits 8 holds the moments as e4m3 codes of m and sqrt(v) with one
+    FP32 scale per 256 values: m[k] and v[k] are then torch.float8_e4m3fn, and
+    the values are m[k].float() * m_scale[k] (each scale repeated 256 times)
+    and the square of v[k].float() * v_scale[k]."""
+
+    def __init__(self, rt, params, grads, lr=6.34e-4, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01,
+                 state_bits=32, copies=None, state=None, steps=0):
+        import torch
+        if state_bits not in (8, 32):
+            raise ValueError("state_bits is 8 or 32")
+        params, grads = list(params), list(grads)
+        copies = list(copies) if copies is not None else [None] * len(params)
+        if not len(params) == len(grads) == len(copies):
+            raise ValueError("params, grads and copies differ in length")
+        gt = grads[0].dtype if grads else torch.float32
+        if gt not in _precisions():
+            raise ValueError(f"gradients are float32 or bfloat16, not {gt}")
+        small = state_bits == 8
+        held = torch.float8_e4m3fn if small else torch.float32
+        blocks = [-(-p.numel() // 256) for p in params]
+        if state is None:
+            new = lambda sizes, t: [torch.zeros(n, dtype=torch.uint8 if t == held and small else t,  # noqa: E731
+                                                device=rt.device).view(t) for n in sizes]
+            sizes = [p.numel() for p in params]
+            state = dict(m=new(sizes, held), v=new(sizes, held))
+            if small:
+                state.update(m_scale=new(blocks, torch.float32), v_scale=new(blocks, torch.float32))
+        self.rt, self.params, self.grads, self.copies = rt, params, grads, copies
+        self.state_bits, self.lr = state_bits, lr
+        self.m, self.v = list(state["m"]), list(state["v"])
+        self.m_scale = list(state["m_scale"]) if small else None
+        self.v_scale = list(state["v_scale"]) if small else None
+        tensors = []
+        for k, (p, g, c) in enumerate(zip(params, grads, copies)):
+            n = p.numel()
+            t = dict(n=n)
+            fields = [("param", p, torch.float32, n), ("grad", g, gt, n), ("copy", c, torch.bfloat16, n),
+                      ("m", self.m[k], held, n), ("v", self.v[k], held, n)]
+            if small:
+                fields += [("m_scale", self.m_scale[k], torch.float32, blocks[k]),
+                           ("v_scale", self.v_scale[k], torch.float32, blocks[k])]
+            for name, a, dtype, size in fields:
+                if a is None:
+                    continue
+                if a.dtype != dtype or a.numel() != size or not a.is_contiguous() or a.device != rt.device:
+                    raise ValueError(f"tensor {k}: {name} must be contiguous {dtype} of {size} values on {rt.device}")
+                t[name] = a.data_ptr() or None
+            tensors.append(t)
+        self.handle = 0
+        cfg = dict(beta1=betas[0], beta2=betas[1], eps=eps, weight_decay=weight_decay, state_bits=state_bits,
+                   grad_precision=B.PAINN_BF16 if gt == torch.bfloat16 else B.PAINN_FP32, steps=steps)
+        cur = rt._enter()
+        self.handle = B.painn_adamw_create(rt.ctx, tensors, cfg)
+        rt._leave(cur, ())
+
+    def step(self, lr=None):
+        """One step on the gradients as they are now, at `lr` or the one given
+        at the start."""
+        cur = self.rt._enter()
+        B.painn_adamw_step(self.rt.ctx, self.handle, self.lr if lr is None else lr)
+        if cur is not None:
+            self.rt._leave(cur, [t for a in (self.params, self.grads, self.copies, self.m, self.v,
+                                             self.m_scale or (), self.v_scale or ()) for t in a if t is not None])
+
+    @property
+    def steps(self):
+        return B.painn_adamw_steps(self.handle)
+
+    def state(self):
+        """The states as they are held, for a later AdamW(..., state=, steps=)."""
+        d = dict(m=self.m, v=self.v)
+        if self.state_bits == 8:
+            d.update(m_scale=self.m_scale, v_scale=self.v_scale)
+        return d
+
+    def free(self):
+        if self.handle and self.rt.ctx:
+            B.painn_adamw_free(self.handle)
+        self.handle = 0
+
+    def __del__(self):
+        if getattr(self, "handle", 0) and sys is not None and not sys.is_finalizing():
+            self.free()
+
+
+_NAMES = {}
+
+
+def _precisions():
+    """torch type -> precision, of the operators for tuning heads."""
+    if not _NAMES:
+        import torch
+        _NAMES.update({torch.float32: B.PAINN_FP32, torch.bfloat16: B.PAINN_BF16})
+    return _NAMES
 
 
 class Runtime:
@@ -184,6 +285,214 @@ class Runtime:
                                  s.data_ptr() if s.numel() else None,
                                  v.data_ptr() if v.numel() else None)
         return s, v
+
+    # ---- operators for tuning heads (FP32, BF16) ---------------------------
+    # They run on the context's stream, like every call; where torch's current
+    # stream is another one, the two wait for each other, so that the caller
+    # sees the order of its own stream.
+    def _enter(self):
+        import torch
+        cur = torch.cuda.current_stream(self.device)
+        if cur == self.stream:
+            return None
+        self.stream.wait_stream(cur)
+        return cur
+
+    def _leave(self, cur, tensors):
+        if cur is None:
+            return
+        for t in tensors:
+            if t is not None:
+                t.record_stream(self.stream)
+        cur.wait_stream(self.stream)
+
+    def _precision(self, x):
+        try:
+            return _precisions()[x.dtype]
+        except KeyError:
+            raise ValueError(f"the operators take float32 or bfloat16, not {x.dtype}") from None
+
+    def _rows(self, t, name, like, rows, cols):
+        """(pointer, row stride) of a matrix whose rows are contiguous."""
+        if t is None:
+            return None, 0
+        if t.dtype != like.dtype or t.device != self.device:
+            raise ValueError(f"{name} must be {like.dtype} on {self.device}, not {t.dtype} on {t.device}")
+        if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+            raise ValueError(f"{name} must be [{rows}, {cols}], not {list(t.shape)}")
+        ld = t.stride(0)
+        if rows <= 1 or cols == 0:
+            ld = max(ld, cols)
+        if (cols > 1 and t.stride(1) != 1) or ld < cols:
+            raise ValueError(f"{name} must have contiguous rows that do not overlap (strides {t.stride()})")
+        return t.data_ptr() or None, ld
+
+    def _whole(self, t, name, dtype, shape):
+        """Pointer of a contiguous tensor."""
+        if t is None:
+            return None
+        if t.dtype != dtype or t.device != self.device or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {list(shape)} on {self.device}, "
+                             f"not {t.dtype} {list(t.shape)} on {t.device}")
+        return t.data_ptr() or None
+
+    def layer_norm(self, x, weight, bias, eps=1e-5, out=None):
+        """(y, mean, rstd) of every row of x [rows, cols]; mean and rstd [rows]
+        are FP32 and go to layer_norm_backward.  `out` may be x."""
+        import torch
+        prec = self._precision(x)
+        if x.dim() != 2:
+            raise ValueError("x must be [rows, cols]")
+        n, c = x.shape
+        px, ldx = self._rows(x, "x", x, n, c)
+        pw, pb = self._whole(weight, "weight", x.dtype, (c,)), self._whole(bias, "bias", x.dtype, (c,))
+        if out is None:
+            out = torch.empty((n, c), dtype=x.dtype, device=self.device)
+        py, ldy = self._rows(out, "out", x, n, c)
+        stats = torch.empty((2, n), dtype=torch.float32, device=self.device)
+        ps = stats.data_ptr()
+        cur = self._enter()
+        B.painn_layer_norm(self.ctx, prec, n, c, px, ldx, pw, pb, eps, py, ldy, ps or None, ps + 4 * n or None)
+        self._leave(cur, (x, weight, bias, out, stats))
+        return out, stats[0], stats[1]
+
+    def layer_norm_backward(self, dy, x, weight, mean, rstd, dx=None, dweight=None, dbias=None, need_dx=True):
+        """(dx, dweight, dbias) from dy and the forward's x, mean and rstd; dx
+        is None without need_dx and may be given as dy."""
+        import torch
+        prec = self._precision(x)
+        if x.dim() != 2:
+            raise ValueError("x must be [rows, cols]")
+        n, c = x.shape
+        px, ldx = self._rows(x, "x", x, n, c)
+        pd, ldd = self._rows(dy, "dy", x, n, c)
+        pw = self._whole(weight, "weight", x.dtype, (c,))
+        pm, pr = (self._whole(t, k, torch.float32, (n,)) for t, k in ((mean, "mean"), (rstd, "rstd")))
+        if need_dx and dx is None:
+            dx = torch.empty((n, c), dtype=x.dtype, device=self.device)
+        dweight = torch.empty_like(weight) if dweight is None else dweight
+        dbias = torch.empty_like(weight) if dbias is None else dbias
+        po, ldo = self._rows(dx, "dx", x, n, c)
+        pg, pb = self._whole(dweight, "dweight", x.dtype, (c,)), self._whole(dbias, "dbias", x.dtype, (c,))
+        cur = self._enter()
+        B.painn_layer_norm_backward(self.ctx, prec, n, c, pd, ldd, px, ldx, pw, pm, pr, po, ldo, pg, pb)
+        self._leave(cur, (dy, x, weight, mean, rstd, dx, dweight, dbias))
+        return dx, dweight, dbias
+
+    def _activation(self, name):
+        try:
+            return B.ACTIVATIONS[name]
+        except KeyError:
+            raise ValueError(f"unknown activation {name!r}: one of {', '.join(B.ACTIVATIONS)}") from None
+
+    def _offsets(self, offsets, groups):
+        import torch
+        return self._whole(offsets, "offsets", torch.int32, (groups + 1,))
+
+    def _dense(self, x, weight, offsets, bias, activation, residual, keep_preact, out):
+        import torch
+        grouped = offsets is not None
+        prec = self._precision(x)
+        if x.dim() != 2 or weight.dim() != (3 if grouped else 2):
+            raise ValueError("x must be [rows, d_in] and weight " + ("[groups, d_out, d_in]" if grouped
+                                                                     else "[d_out, d_in]"))
+        n, i = x.shape
+        lead, o = tuple(weight.shape[:-2]), weight.shape[-2]
+        a = B.painn_linear_args(precision=prec, activation=self._activation(activation), rows=n, d_in=i, d_out=o)
+        a.x, a.ldx = self._rows(x, "x", x, n, i)
+        a.w = self._whole(weight, "weight", x.dtype, lead + (o, i))
+        a.bias = self._whole(bias, "bias", x.dtype, lead + (o,))
+        a.residual, a.ldr = self._rows(residual, "residual", x, n, o)
+        if out is None:
+            out = torch.empty((n, o), dtype=x.dtype, device=self.device)
+        a.y, a.ldy = self._rows(out, "out", x, n, o)
+        z = torch.empty((n, o), dtype=x.dtype, device=self.device) if keep_preact else None
+        a.z, a.ldz = self._rows(z, "z", x, n, o)
+        po = self._offsets(offsets, lead[0]) if grouped else None
+        cur = self._enter()
+        if grouped:
+            B.painn_grouped_linear(self.ctx, a, lead[0], po)
+        else:
+            B.painn_linear(self.ctx, a)
+        self._leave(cur, (x, weight, offsets, bias, residual, out, z))
+        return (out, z) if keep_preact else out
+
+    def linear(self, x, weight, bias=None, activation="none", residual=None, keep_preact=False, out=None):
+        """y = activation(x weight^T + bias) + residual; x [rows, d_in], weight
+        [d_out, d_in].  keep_preact: (y, z), z the activation's input, for
+        linear_backward.  `residual` may be `out`."""
+        return self._dense(x, weight, None, bias, activation, residual, keep_preact, out)
+
+    def grouped_linear(self, x, weight, offsets, bias=None, activation="none", residual=None, keep_preact=False,
+                       out=None):
+        """linear with weight [groups, d_out, d_in] and bias [groups, d_out]:
+        group g has the rows offsets[g] .. offsets[g+1] (int32 on the GPU).
+        Rows of no group are left as they are in `out` (undefined in a new
+        one)."""
+        if offsets is None:
+            raise ValueError("offsets is missing")
+        return self._dense(x, weight, offsets, bias, activation, residual, keep_preact, out)
+
+    def _dense_backward(self, dy, x, weight, offsets, activation, preact, x_activation, x_preact, need_dx, dx,
+                        dweight, dbias):
+        import torch
+        grouped = offsets is not None
+        prec = self._precision(x)
+        if x.dim() != 2 or weight.dim() != (3 if grouped else 2):
+            raise ValueError("x must be [rows, d_in] and weight " + ("[groups, d_out, d_in]" if grouped
+                                                                     else "[d_out, d_in]"))
+        n, i = x.shape
+        lead, o = tuple(weight.shape[:-2]), weight.shape[-2]
+        a = B.painn_linear_backward_args(precision=prec, activation=self._activation(activation), rows=n, d_in=i,
+                                         d_out=o, x_activation=self._activation(x_activation))
+        if a.activation and preact is None:
+            raise ValueError(f"preact is missing for activation {activation!r}")
+        if a.x_activation and need_dx and x_preact is None:
+            raise ValueError(f"x_preact is missing for x_activation {x_activation!r}")
+        a.dy, a.lddy = self._rows(dy, "dy", x, n, o)
+        a.z, a.ldz = self._rows(preact, "preact", x, n, o)
+        a.x, a.ldx = self._rows(x, "x", x, n, i)
+        a.w = self._whole(weight, "weight", x.dtype, lead + (o, i))
+        a.xz, a.ldxz = self._rows(x_preact, "x_preact", x, n, i)
+        if need_dx and dx is None:
+            dx = torch.empty((n, i), dtype=x.dtype, device=self.device)
+        if dweight is None:
+            dweight = torch.empty_like(weight)
+        if dbias is None:
+            dbias = torch.empty(lead + (o,), dtype=x.dtype, device=self.device)
+        a.dx, a.lddx = self._rows(dx, "dx", x, n, i)
+        a.dw = self._whole(dweight, "dweight", x.dtype, lead + (o, i))
+        a.dbias = self._whole(dbias, "dbias", x.dtype, lead + (o,))
+        po = self._offsets(offsets, lead[0]) if grouped else None
+        cur = self._enter()
+        if grouped:
+            B.painn_grouped_linear_backward(self.ctx, a, lead[0], po)
+        else:
+            B.painn_linear_backward(self.ctx, a)
+        self._leave(cur, (dy, x, weight, offsets, preact, x_preact, dx, dweight, dbias))
+        return dx, dweight, dbias
+
+    def linear_backward(self, dy, x, weight, activation="none", preact=None, x_activation="none", x_preact=None,
+                        need_dx=True, dx=None, dweight=None, dbias=None):
+        """(dx, dweight, dbias) of linear.  preact: the forward's z, needed with
+        an activation.  With x_activation and x_preact (x =
+        x_activation(x_preact)), dx is the gradient of x_preact.  The
+        residual's gradient is dy."""
+        return self._dense_backward(dy, x, weight, None, activation, preact, x_activation, x_preact, need_dx, dx,
+                                    dweight, dbias)
+
+    def grouped_linear_backward(self, dy, x, weight, offsets, activation="none", preact=None, x_activation="none",
+                                x_preact=None, need_dx=True, dx=None, dweight=None, dbias=None):
+        """linear_backward of grouped_linear; dweight and dbias of a group
+        without rows are zero."""
+        if offsets is None:
+            raise ValueError("offsets is missing")
+        return self._dense_backward(dy, x, weight, offsets, activation, preact, x_activation, x_preact, need_dx, dx,
+                                    dweight, dbias)
+
+    def adamw(self, params, grads, **how) -> AdamW:
+        """An optimizer of these tensors (AdamW's arguments)."""
+        return AdamW(self, params, grads, **how)
 
     def synchronize(self):
         B.painn_synchronize(self.ctx)
