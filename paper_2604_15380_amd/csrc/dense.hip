@@ -85,15 +85,15 @@ __device__ __forceinline__ Span find_tile(const Groups& gr, int t, int len, int 
     if (past) {
       const int l = __ffsll((long long)past) - 1;
       s.g = g0 + l;
-      s.count = __shfl(tiles, l);
-      s.index = t - (__shfl(end, l) - s.count);
-      s.lo = __shfl((int)lo, l);
-      s.hi = __shfl((int)hi, l);
+      s.count = __builtin_amdgcn_readlane(tiles, l);
+      s.index = t - (__builtin_amdgcn_readlane(end, l) - s.count);
+      s.lo = __builtin_amdgcn_readlane((int)lo, l);
+      s.hi = __builtin_amdgcn_readlane((int)hi, l);
       // (offsets that decrease may count more tiles than there are)
       if (s.index < 0 || s.index >= s.count) s.g = -1;
       return s;
     }
-    before = __shfl(end, 63);
+    before = __builtin_amdgcn_readlane(end, 63);
   }
   return s;
 }
@@ -257,46 +257,149 @@ struct Args {
   int tiles;                         // FWD, DX: row tiles (an upper bound); DW: chunks
   int nt;                            // column tiles of a row tile; DW: tiles of dw
   int nt_in;                         // DW: tiles along d_in
+  bool past, past_z;                 // whether out and z are stored past the caches
 };
+
+// A block's tile: rows [m0, m_end) of A from a, rows [n0, n_end) of B from b, nk
+// values of k.
+template <class T>
+struct Tile {
+  Span s;
+  int t;                      // row tile or chunk
+  const T *a, *b;
+  long long m0, m_end, n0, n_end, nk;
+};
+
+template <class T, int BM, int BN, int MODE>
+__device__ __forceinline__ bool locate(const Args& g, Tile<T>& w) {
+  // Many row tiles: the column tiles of one on one XCD, next to each other, so
+  // that its rows are read from that L2.  Few: all tiles over all XCDs.  (DW:
+  // the tiles of one chunk; its rows are most of what the pass reads.)
+  const bool many = g.tiles >= (MODE == DW ? 8 : 64);
+  const int lin = many ? blockIdx.x >> 3 : blockIdx.x;
+  const int c = lin % g.nt;
+  w.t = many ? (lin / g.nt) * 8 + (blockIdx.x & 7) : lin / g.nt;
+  if (w.t >= g.tiles) return false;
+  w.s = find_tile(g.gr, w.t, MODE == DW ? g.chunk : BM, MODE == DW ? 1 : 0);
+  if (w.s.g < 0) return false;
+  w.a = (const T*)g.a;
+  w.b = (const T*)g.b;
+  if constexpr (MODE == DW) {
+    const long long lo = w.s.lo + (long long)w.s.index * g.chunk;
+    w.nk = w.s.hi - lo < g.chunk ? w.s.hi - lo : g.chunk;
+    w.a += lo * g.lda;
+    w.b += lo * g.ldb;
+    w.m0 = (long long)(c / g.nt_in) * BM;
+    w.n0 = (long long)(c % g.nt_in) * BN;
+    w.m_end = g.d_out;
+    w.n_end = g.d_in;
+  } else {
+    w.m0 = w.s.lo + (long long)w.s.index * BM;
+    w.m_end = w.s.hi;
+    w.n0 = (long long)c * BN;
+    w.n_end = MODE == FWD ? g.d_out : g.d_in;
+    w.nk = MODE == FWD ? g.d_in : g.d_out;
+    w.b += (size_t)w.s.g * g.d_out * g.d_in;
+  }
+  return true;
+}
+
+// The tile's results.  A lane holds, per fragment, row l % 16 and the columns
+// 4 (l / 16) .. + 3; stored like that, a wave would write 32 bytes per row.
+// So each wave passes 16 rows at a time through its own piece of LDS and takes
+// them back as 8 neighbouring columns per lane: bias, activation, residual and
+// all loads and stores work on whole rows of the wave's tile.  wm, wn: the
+// wave's corner in the tile; lds: finish_floats per wave, free for use.
+template <int FN> constexpr int finish_floats() { return 16 * (FN * 16 + 4); }
+
+template <class T, int FM, int FN, int MODE>
+__device__ __forceinline__ void finish(const Args& g, const Tile<T>& w, int wm, int wn, const f4_t (&acc)[FM][FN],
+                                       const f4_t* accb, bool sum_b, float* lds) {
+  constexpr int WT = FN * 16, PITCH = WT + 4, LPR = WT / 8, RPP = 64 / LPR;     // lanes per row, rows per pass
+  const int lane = threadIdx.x & 63, lr = lane & 15, lq = lane >> 4;
+  float* my = lds + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * finish_floats<FN>();
+  const size_t wsize = (size_t)g.d_out * g.d_in;
+  const long long n = w.n0 + wn + (lane % LPR) * 8, left = w.n_end - n;
+  const bool whole = MODE != DW || w.s.count == 1;
+  T* out = (T*)g.out + (MODE == DW ? (size_t)w.s.g * wsize : 0) + n;
+  float* part = MODE == DW && !whole ? g.part + (size_t)w.t * wsize + n : nullptr;
+  const long long ldo = MODE == DW ? g.d_in : g.ldo;
+  float bias[8];
+  if (MODE == FWD && g.bias) load_n<8>((const T*)g.bias + (size_t)w.s.g * g.d_out + n, left, bias);
+#pragma unroll
+  for (int i = 0; i < FM; ++i) {
+#pragma unroll
+    for (int j = 0; j < FN; ++j) *(f4_t*)(my + lr * PITCH + 16 * j + 4 * lq) = acc[i][j];
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int q = 0; q < (16 + RPP - 1) / RPP; ++q) {
+      const int r = q * RPP + lane / LPR;
+      const long long m = w.m0 + wm + 16 * i + r;
+      if (lane < LPR * RPP && r < 16 && m < w.m_end && left > 0) {
+        float v[8];
+        const f4_t x = *(const f4_t*)(my + r * PITCH + (lane % LPR) * 8);
+        const f4_t y = *(const f4_t*)(my + r * PITCH + (lane % LPR) * 8 + 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          v[e] = x[e];
+          v[4 + e] = y[e];
+        }
+        if constexpr (MODE == DW) {
+          if (!whole) {
+            store_n<8>(part + m * ldo, left, v);
+            continue;
+          }
+        } else if constexpr (MODE == FWD) {
+          if (g.bias) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += bias[e];
+          }
+          if (g.z) {
+            if (g.past_z && left >= 8) store_past<8>((T*)g.z + m * g.ldz + n, v);
+            else store_n<8>((T*)g.z + m * g.ldz + n, left, v);
+          }
+          act<8>(v, g.act);
+          if (g.e) {
+            float res[8];
+            load_n<8>((const T*)g.e + m * g.lde + n, left, res);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += res[e];
+          }
+        } else if (g.act != PAINN_ACT_NONE) {
+          float z[8];
+          load_n<8>((const T*)g.e + m * g.lde + n, left, z);
+          mul_slope<8>(v, z, g.act);
+        }
+        if (MODE != DW && g.past && left >= 8) store_past<8>(out + m * ldo, v);
+        else store_n<8>(out + m * ldo, left, v);
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+    if constexpr (MODE == DW) {
+      const long long m = w.m0 + wm + 16 * i + lr;
+      if (sum_b && lq == 0 && m < w.m_end) {
+        const float v = accb[i][0];
+        if (whole) store<1>((T*)g.db + (size_t)w.s.g * g.d_out + m, &v);
+        else g.part_b[(size_t)w.t * g.d_out + m] = v;
+      }
+    }
+  }
+}
 
 template <class T, int BM, int BN, int WM, int WN, int MODE>
 __global__ void __launch_bounds__(64 * WM * WN, 2) k_dense(Args g) {
   using M = Mma<T>;
   constexpr int NP = M::NP, BK = M::BK, TH = 64 * WM * WN;
   constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
-  __shared__ __attribute__((aligned(16))) uint16_t As[NP * BM * BK], Bs[NP * BN * BK];
-  // Many row tiles: the column tiles of one on one XCD, next to each other, so
-  // that its rows are read from that L2.  Few: all tiles over all XCDs.
-  const bool many = g.tiles >= 64;
-  const int lin = many ? blockIdx.x >> 3 : blockIdx.x;
-  const int t = many ? (lin / g.nt) * 8 + (blockIdx.x & 7) : lin / g.nt, c = lin % g.nt;
-  if (t >= g.tiles) return;
-  const Span s = find_tile(g.gr, t, MODE == DW ? g.chunk : BM, MODE == DW ? 1 : 0);
-  if (s.g < 0) return;
-
-  const T *a = (const T*)g.a, *b = (const T*)g.b;
-  const size_t wsize = (size_t)g.d_out * g.d_in;
-  long long m0, m_end, n0, n_end, nk;
-  if constexpr (MODE == DW) {
-    const long long lo = s.lo + (long long)s.index * g.chunk;
-    nk = s.hi - lo < g.chunk ? s.hi - lo : g.chunk;
-    a += lo * g.lda;
-    b += lo * g.ldb;
-    m0 = (long long)(c / g.nt_in) * BM;
-    n0 = (long long)(c % g.nt_in) * BN;
-    m_end = g.d_out;
-    n_end = g.d_in;
-  } else {
-    m0 = s.lo + (long long)s.index * BM;
-    m_end = s.hi;
-    n0 = (long long)c * BN;
-    n_end = MODE == FWD ? g.d_out : g.d_in;
-    nk = MODE == FWD ? g.d_in : g.d_out;
-    b += (size_t)s.g * wsize;
-  }
+  constexpr int SA = NP * BM * BK, SB = NP * BN * BK;
+  static_assert((SA + SB) * 2 >= WM * WN * finish_floats<FN>() * 4, "room for finish");
+  __shared__ __attribute__((aligned(16))) uint16_t As[SA + SB];
+  uint16_t* Bs = As + SA;
+  Tile<T> w;
+  if (!locate<T, BM, BN, MODE>(g, w)) return;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, lr = lane & 15, lq = lane >> 4;
   const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
-  const bool sum_b = MODE == DW && g.db != nullptr && n0 == 0 && wn == 0;
+  const bool sum_b = MODE == DW && g.db != nullptr && w.n0 == 0 && wn == 0;
 
   f4_t acc[FM][FN], accb[MODE == DW ? FM : 1];
 #pragma unroll
@@ -311,17 +414,18 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_dense(Args g) {
 
   Stage<T, BM, TH, MODE == DW> sa;
   Stage<T, BN, TH, MODE != FWD> sb;
+  const long long nk = w.nk;
   if (nk > 0) {
-    sa.load(a, g.lda, m0, m_end, 0, nk);
-    sb.load(b, g.ldb, n0, n_end, 0, nk);
+    sa.load(w.a, g.lda, w.m0, w.m_end, 0, nk);
+    sb.load(w.b, g.ldb, w.n0, w.n_end, 0, nk);
   }
   for (long long k0 = 0; k0 < nk; k0 += BK) {
     sa.put(As);
     sb.put(Bs);
     __syncthreads();
     if (k0 + BK < nk) {
-      sa.load(a, g.lda, m0, m_end, k0 + BK, nk);
-      sb.load(b, g.ldb, n0, n_end, k0 + BK, nk);
+      sa.load(w.a, g.lda, w.m0, w.m_end, k0 + BK, nk);
+      sb.load(w.b, g.ldb, w.n0, w.n_end, k0 + BK, nk);
     }
 #pragma unroll
     for (int kk = 0; kk < BK / 32; ++kk) {
@@ -359,72 +463,185 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_dense(Args g) {
     }
     __syncthreads();
   }
+  finish<T, FM, FN, MODE>(g, w, wm, wn, acc, accb, sum_b, (float*)As);
+}
 
-  if constexpr (MODE == DW) {
-    const bool whole = s.count == 1;
-    float* part = whole ? nullptr : g.part + (size_t)t * wsize;
-    T* out = (T*)g.out + (size_t)s.g * wsize;
+// ---- BF16 operands in 16-byte words -------------------------------------------------
+// Where every row of the operands starts at a multiple of 16 bytes and the
+// widths are multiples of 8, the k-blocks go from memory to LDS without
+// passing registers (16 bytes per lane, the lanes of a wave next to each other
+// in LDS), into the buffer that is not being read.  Words past the last k
+// come from a word of zeros.  A plain operand lies as [row][64] with its
+// 16-byte chunks permuted by the row; a transposed one stays [k][row] with its
+// chunks permuted by k and is turned by the transposing LDS reads, 4 k x 16
+// rows at a time (lane l asks for k = l / 4 % 4 and rows 4 (l % 4) .. + 3 of
+// its 16 lanes' block and receives 4 k of row l % 16).
+__device__ const u4_t zero_word = {0, 0, 0, 0};
+
+typedef short s4_t __attribute__((ext_vector_type(4)));
+
+// 16 bytes per lane from p to LDS, the lanes one after the other from byte `at`
+// (the same for the wave).  Written as an instruction because the compiler
+// would wait for it before any LDS read, the other buffer's too: it knows
+// nothing of it, and wait_loads() does the waiting.  (It has no register
+// output that could be taken too early.)
+__device__ __forceinline__ void load_to_lds(const void* p, uint32_t at) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(p), "s"(at) : "memory");
+}
+__device__ __forceinline__ uint32_t lds_byte(const void* p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
+}
+// All of this wave's loads are done, those to LDS among them.
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" : : : "memory"); }
+
+template <int R, int BK, int TH, bool TR>
+struct Dma {
+  static constexpr int CH = BK / 8, C = R / 8, UNITS = R * BK / 8, U = (UNITS + TH - 1) / TH;
+  static constexpr int READS = TR ? 2 : 1;      // LDS reads of a fragment
+  static_assert(UNITS % 64 == 0, "whole waves of words");
+  const b16* base;             // of the next k-block, the same for all lanes
+  uint32_t off[U];             // this lane's words in it
+
+  // plain: how row `row`'s chunks are permuted, so that 8 rows' words of one
+  // chunk lie in different banks
+  __device__ __forceinline__ static int turn(int row) { return CH == 8 ? row & 7 : (row >> 1) & 3; }
+  // transposed: chunk c of k's row lies at (c + 2 (k % 4)) % C; the reverse
+  __device__ __forceinline__ static int row_chunk(int at, int k) {
+    const int c = at - 2 * (k & 3);
+    return c < 0 ? c + C : c;
+  }
+  // the word's first k in the k-block
+  __device__ __forceinline__ static int first_k(int i) {
+    const int u = i * TH + threadIdx.x;
+    if constexpr (TR) return u / C;
+    return ((u % CH) ^ turn(u / CH)) * 8;
+  }
+  // Rows [r0, r0 + R) of n_rows (at least 1; transposed: a multiple of 8) of a
+  // matrix whose row stride is below 2^22.  Rows past n_rows hold others' values.
+  __device__ __forceinline__ void init(const b16* m, long long ld, long long r0, long long n_rows) {
+    const int most = (int)(n_rows - r0 < R ? n_rows - r0 : R) - (TR ? 8 : 1);
+    base = TR ? m + r0 : m + r0 * ld;
 #pragma unroll
-    for (int i = 0; i < FM; ++i) {
-      const long long m = m0 + wm + 16 * i + lr;
-      if (m >= m_end) continue;
-#pragma unroll
-      for (int j = 0; j < FN; ++j) {
-        const long long n = n0 + wn + 16 * j + 4 * lq;
-        if (n >= n_end) continue;
-        float v[4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] = acc[i][j][r];
-        if (whole) store_n<4>(out + m * g.d_in + n, n_end - n, v);
-        else store_n<4>(part + m * g.d_in + n, n_end - n, v);
-      }
-      if (sum_b && lq == 0) {
-        const float v = accb[i][0];
-        if (whole) store<1>((T*)g.db + (size_t)s.g * g.d_out + m, &v);
-        else g.part_b[(size_t)t * g.d_out + m] = v;
-      }
-    }
-  } else {
-    float bias[FN][4];
-    if constexpr (MODE == FWD) {
-#pragma unroll
-      for (int j = 0; j < FN; ++j) {
-        const long long n = n0 + wn + 16 * j + 4 * lq;
-        if (g.bias) load_n<4>((const T*)g.bias + (size_t)s.g * g.d_out + n, n_end - n, bias[j]);
-        else bias[j][0] = bias[j][1] = bias[j][2] = bias[j][3] = 0.f;
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < FM; ++i) {
-      const long long m = m0 + wm + 16 * i + lr;
-      if (m >= m_end) continue;
-#pragma unroll
-      for (int j = 0; j < FN; ++j) {
-        const long long n = n0 + wn + 16 * j + 4 * lq, left = n_end - n;
-        if (left <= 0) continue;
-        float v[4], e[4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] = acc[i][j][r];
-        if constexpr (MODE == FWD) {
-#pragma unroll
-          for (int r = 0; r < 4; ++r) v[r] += bias[j][r];
-          if (g.z) store_n<4>((T*)g.z + m * g.ldz + n, left, v);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) v[r] = act(v[r], g.act);
-          if (g.e) {
-            load_n<4>((const T*)g.e + m * g.lde + n, left, e);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) v[r] += e[r];
-          }
-        } else if (g.act != PAINN_ACT_NONE) {
-          load_n<4>((const T*)g.e + m * g.lde + n, left, e);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) v[r] *= act_slope(e[r], g.act);
-        }
-        store_n<4>((T*)g.out + m * g.ldo + n, left, v);
-      }
+    for (int i = 0; i < U; ++i) {
+      const int u = i * TH + threadIdx.x, k = first_k(i);
+      int r = TR ? row_chunk(u % C, k) * 8 : u / CH;
+      r = r < most ? r : most;
+      off[i] = TR ? k * (uint32_t)ld + r : r * (uint32_t)ld + k;
     }
   }
+  // The next k-block, `left` values of k from its start on, to lds.
+  __device__ __forceinline__ void next(uint16_t* lds, long long ld, long long left) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t at = lds_byte(lds) + wave * 1024;
+    const bool whole = left >= BK;
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      if (UNITS % TH != 0 && i * TH + wave * 64 >= UNITS) break;
+      if (whole) load_to_lds(base + off[i], at + i * TH * 16);
+      else load_to_lds(first_k(i) < left ? base + off[i] : (const b16*)&zero_word, at + i * TH * 16);
+    }
+    base += TR ? BK * ld : BK;
+  }
+  // The fragment of rows [r, r + 16) and 32 k from 32 kk on.
+  __device__ __forceinline__ static bf8_t frag(const uint16_t* lds, int r, int kk) {
+    const int lane = threadIdx.x & 63, lr = lane & 15, lq = lane >> 4;
+    if constexpr (!TR) {
+      return *(const bf8_t*)(lds + (r + lr) * BK + (((4 * kk + lq) ^ turn(lr)) << 3));
+    } else {
+      const int k = 32 * kk + 8 * lq + (lr >> 2);
+      int c = (r >> 3) + ((lr & 3) >> 1) + 2 * (k & 3);
+      c = c < C ? c : c - C;
+      const uint16_t* a = lds + k * R + c * 8 + 4 * (lr & 1);
+      const s4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4_t*)a);
+      const s4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4_t*)(a + 4 * R));
+      typedef short s8_t __attribute__((ext_vector_type(8)));
+      const s8_t v = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+      return __builtin_bit_cast(bf8_t, v);
+    }
+  }
+};
+
+template <int BM, int BN, int WM, int WN, int MODE>
+__global__ void __launch_bounds__(64 * WM * WN, 2) k_dense16(Args g) {
+  constexpr int TH = 64 * WM * WN, BK = 64, NB = 2;
+  constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
+  using A = Dma<BM, BK, TH, MODE == DW>;
+  using B = Dma<BN, BK, TH, MODE != FWD>;
+  constexpr int SA = BM * BK, SB = BN * BK;
+  static_assert(NB * (SA + SB) * 2 >= WM * WN * finish_floats<FN>() * 4, "room for finish");
+  __shared__ __attribute__((aligned(16))) uint16_t lds[NB][SA + SB];
+  Tile<b16> w;
+  if (!locate<b16, BM, BN, MODE>(g, w)) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
+  const bool sum_b = MODE == DW && g.db != nullptr && w.n0 == 0 && wn == 0;
+
+  f4_t acc[FM][FN], accb[MODE == DW ? FM : 1];
+#pragma unroll
+  for (int i = 0; i < FM; ++i) {
+    if constexpr (MODE == DW) accb[i] = f4_t{0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < FN; ++j) acc[i][j] = f4_t{0, 0, 0, 0};
+  }
+  bf8_t ones;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) ones[i] = (b16)1.f;
+
+  A sa;
+  B sb;
+  sa.init(w.a, g.lda, w.m0, w.m_end);
+  sb.init(w.b, g.ldb, w.n0, w.n_end);
+  long long left = w.nk;                // k from the block being read on
+  auto fetch = [&](int buf, long long from) {
+    sa.next(lds[buf], g.lda, from);
+    sb.next(lds[buf] + SA, g.ldb, from);
+  };
+  if (left > 0) fetch(0, left);
+  for (int cur = 0; left > 0; cur ^= 1, left -= BK) {
+    // everybody's words of this block are there, and nobody reads the other buffer
+    wait_loads();
+    __syncthreads();
+    if (left > BK) fetch(cur ^ 1, left - BK);
+    const uint16_t *a = lds[cur], *b = a + SA;
+    bf8_t fa[2][FM], fb[2][FN];
+    auto read = [&](int kk) {
+#pragma unroll
+      for (int j = 0; j < FN; ++j) fb[kk][j] = B::frag(b, wn + 16 * j, kk);
+#pragma unroll
+      for (int i = 0; i < FM; ++i) fa[kk][i] = A::frag(a, wm + 16 * i, kk);
+    };
+    auto multiply = [&](int kk) {
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[kk][j], fa[kk][i], acc[i][j], 0, 0, 0);
+      if constexpr (MODE == DW)
+        if (sum_b) {
+          // the column sums of dz, as a product with ones
+#pragma unroll
+          for (int i = 0; i < FM; ++i)
+            accb[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, fa[kk][i], accb[i], 0, 0, 0);
+        }
+    };
+    // The second half's fragments are read between the first half's products,
+    // a read to every few products; left to itself the compiler reads a few
+    // and waits for them, over and over.
+    constexpr int READS = FM * A::READS + FN * B::READS, PER = FM * FN / READS > 0 ? FM * FN / READS : 1;
+    read(0);
+    __builtin_amdgcn_sched_barrier(0);
+    read(1);
+    multiply(0);
+#pragma unroll
+    for (int q = 0; q < READS; ++q) {
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);       // LDS reads
+      __builtin_amdgcn_sched_group_barrier(0x008, PER, 0);     // matrix products
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    multiply(1);
+  }
+  __syncthreads();
+  finish<b16, FM, FN, MODE>(g, w, wm, wn, acc, accb, sum_b, (float*)lds);
 }
 
 // dz = dy activation'(z), [rows][d_out] without gaps.
@@ -440,8 +657,7 @@ __global__ void __launch_bounds__(256) k_dz(long long rows, int d_out, const T* 
   float d[V], s[V];
   load_n<V>(dy + r * lddy + c, d_out - c, d);
   load_n<V>(z + r * ldz + c, d_out - c, s);
-#pragma unroll
-  for (int k = 0; k < V; ++k) d[k] *= act_slope(s[k], kind);
+  mul_slope<V>(d, s, kind);
   store_n<V>(dz + r * d_out + c, d_out - c, d);
 }
 
@@ -496,13 +712,36 @@ inline long long tile_bound(const Groups& gr, int len, int least) {
   return gr.n ? n + gr.n : n < least ? least : n;
 }
 
+// Whether an operand's rows can be read in 16-byte words.
+inline bool words(const void* p, long long ld, int width) {
+  return (uintptr_t)p % 16 == 0 && ld % 8 == 0 && ld < (1 << 22) && width % 8 == 0;
+}
+
+// Whether an output is stored past the caches: where it is larger than the
+// L2s (8 x 4 MB), so that it does not drive the operands out of them, and its
+// rows are whole 128-byte lines; a line written in two parts would go to
+// memory twice.  (65,536 x 1,024 -> 1,024, SiLU, z kept: 171 -> 151 us; at 776
+// columns, rows of 12 1/8 lines, 159 -> 172 us.)
+inline bool past_caches(const void* p, long long ld, long long rows, size_t es) {
+  return (uintptr_t)p % 128 == 0 && ld * es % 128 == 0 && rows * ld * es > (32 << 20);
+}
+
 template <class T, int BM, int BN, int WM, int WN, int MODE>
 bool launch(hipStream_t st, Args a, long long tiles, long long nt) {
   if (tiles > 0x7fffffffLL / (nt < 8 ? 8 : nt) - 8) return false;
-  const long long blocks = (tiles >= 64 ? ceil_div(tiles, 8) * 8 : tiles) * nt;
+  const long long blocks = (tiles >= (MODE == DW ? 8 : 64) ? ceil_div(tiles, 8) * 8 : tiles) * nt;
   if (blocks == 0) return true;
   a.tiles = (int)tiles;
   a.nt = (int)nt;
+  a.past = past_caches(a.out, a.ldo, a.gr.rows, sizeof(T));
+  a.past_z = past_caches(a.z, a.ldz, a.gr.rows, sizeof(T));
+  if constexpr (sizeof(T) == 2) {
+    if (words(a.a, a.lda, MODE == FWD ? a.d_in : a.d_out) && words(a.b, a.ldb, a.d_in) &&
+        (size_t)a.d_out * a.d_in % 8 == 0) {
+      k_dense16<BM, BN, WM, WN, MODE><<<dim3((unsigned)blocks), 64 * WM * WN, 0, st>>>(a);
+      return true;
+    }
+  }
   k_dense<T, BM, BN, WM, WN, MODE><<<dim3((unsigned)blocks), 64 * WM * WN, 0, st>>>(a);
   return true;
 }
@@ -551,7 +790,7 @@ painn_status run_bwd(painn_ctx* ctx, const painn_linear_backward_args& p, int n_
   const bool big = p.d_in > 64 && p.d_out > 64;
   const int bt = big ? 128 : 64;
   const long long nt = ceil_div(p.d_out, bt) * ceil_div(p.d_in, bt);
-  const long long want = ceil_div(FULL, nt);
+  const long long fit = FULL / nt > 1 ? FULL / nt : 1, want = fit < 8 ? fit : fit / 8 * 8;   // (8 XCDs)
   const long long chunk = ((ceil_div(p.rows, want) + 255) / 256) * 256;
   a.chunk = (int)(chunk < 256 ? 256 : chunk > (1 << 24) ? 1 << 24 : chunk);
   const long long slots = tile_bound(a.gr, a.chunk, 1);

@@ -65,6 +65,21 @@ __device__ __forceinline__ void store(b16* p, const float* x) {
   for (int i = 0; i < V; ++i) v[i] = (b16)x[i];
   *(typename Pack<b16, V>::type*)p = v;
 }
+// Store 16-byte words past the caches, for outputs much larger than they are.
+template <int V, class T>
+__device__ __forceinline__ void store_past(T* p, const float* x) {
+  typedef uint32_t word __attribute__((ext_vector_type(4)));
+  constexpr int E = 16 / sizeof(T);
+#pragma unroll
+  for (int k = 0; k < V / E; ++k) {
+    T v[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) v[i] = (T)x[k * E + i];
+    word w;
+    __builtin_memcpy(&w, v, 16);
+    __builtin_nontemporal_store(w, (word*)(p + k * E));
+  }
+}
 // The first n of V values (n may be <= 0 or above V); what is not loaded is 0.
 template <int V, class T>
 __device__ __forceinline__ void load_n(const T* p, long long n, float* x) {
@@ -96,22 +111,43 @@ __device__ __forceinline__ float wave_sum(float x) {
   return x;
 }
 
-// activation(z) and its derivative, as written in painn.h
-__device__ __forceinline__ float act(float z, int kind) {
-  if (kind == PAINN_ACT_SILU) return z / (1.f + expf(-z));
-  if (kind == PAINN_ACT_RELU) return z < 0.f ? 0.f : z;
-  if (kind == PAINN_ACT_GELU) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
-  return z;
-}
-__device__ __forceinline__ float act_slope(float z, int kind) {
+// activation(z) and its derivative, as written in painn.h.  The exponentials
+// and reciprocals are the hardware's (1 ulp): exp(-z) is off by |z| 2^-24 of
+// itself, which leaves a sigmoid within 2^-23 absolute.
+__device__ __forceinline__ float fast_exp(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
+__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + fast_exp(-z)); }
+
+template <int N>
+__device__ __forceinline__ void act(float* z, int kind) {
   if (kind == PAINN_ACT_SILU) {
-    const float s = 1.f / (1.f + expf(-z));
-    return s * (1.f + z * (1.f - s));
+#pragma unroll
+    for (int i = 0; i < N; ++i) z[i] *= sigmoid(z[i]);
+  } else if (kind == PAINN_ACT_RELU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) z[i] = z[i] < 0.f ? 0.f : z[i];
+  } else if (kind == PAINN_ACT_GELU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) z[i] = 0.5f * z[i] * (1.f + erff(z[i] * 0.70710678118654752f));
   }
-  if (kind == PAINN_ACT_RELU) return z > 0.f ? 1.f : 0.f;
-  if (kind == PAINN_ACT_GELU)
-    return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * expf(-0.5f * z * z) * 0.39894228040143268f;
-  return 1.f;
+}
+// x *= activation'(z)
+template <int N>
+__device__ __forceinline__ void mul_slope(float* x, const float* z, int kind) {
+  if (kind == PAINN_ACT_SILU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float s = sigmoid(z[i]);
+      x[i] *= s * (1.f + z[i] * (1.f - s));
+    }
+  } else if (kind == PAINN_ACT_RELU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] *= z[i] > 0.f ? 1.f : 0.f;
+  } else if (kind == PAINN_ACT_GELU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      x[i] *= 0.5f * (1.f + erff(z[i] * 0.70710678118654752f)) +
+              z[i] * fast_exp(-0.5f * z[i] * z[i]) * 0.39894228040143268f;
+  }
 }
 
 }  // namespace ops
