@@ -38,7 +38,6 @@ struct Groups {
 struct Span {
   int g;                        // group, -1: none
   int index;                    // tile within the group
-  int count;                    // tiles of the group
   long long lo, hi;             // rows of the group
 };
 
@@ -50,18 +49,12 @@ __device__ __forceinline__ void group_rows(const Groups& gr, int g, long long& l
   hi = hi < lo ? lo : hi > gr.rows ? gr.rows : hi;
 }
 
-// Tile t of all groups' tiles of `len` rows, at least `least` per group.  Every
-// wave of the block finds the same.
-__device__ __forceinline__ Span find_tile(const Groups& gr, int t, int len, int least) {
-  Span s{-1, 0, 0, 0, 0};
+// Tile t of all groups' tiles of `len` rows.  Every wave of the block finds the
+// same.
+__device__ __forceinline__ Span find_tile(const Groups& gr, int t, int len) {
+  Span s{-1, 0, 0, 0};
   if (gr.n == 0) {
-    const int tiles = (int)((gr.rows + len - 1) / len);
-    s.count = tiles < least ? least : tiles;
-    if (t < s.count) {
-      s.g = 0;
-      s.index = t;
-      s.hi = gr.rows;
-    }
+    if ((long long)t * len < gr.rows) s = Span{0, t, 0, gr.rows};
     return s;
   }
   const int lane = threadIdx.x & 63;
@@ -72,7 +65,6 @@ __device__ __forceinline__ Span find_tile(const Groups& gr, int t, int len, int 
     if (g0 + lane < gr.n) {
       group_rows(gr, g0 + lane, lo, hi);
       tiles = (int)((hi - lo + len - 1) / len);
-      tiles = tiles < least ? least : tiles;
     }
     int end = tiles;
 #pragma unroll
@@ -84,18 +76,26 @@ __device__ __forceinline__ Span find_tile(const Groups& gr, int t, int len, int 
     const unsigned long long past = __ballot(t < end);
     if (past) {
       const int l = __ffsll((long long)past) - 1;
-      s.g = g0 + l;
-      s.count = __builtin_amdgcn_readlane(tiles, l);
-      s.index = t - (__builtin_amdgcn_readlane(end, l) - s.count);
+      s.index = t - (__builtin_amdgcn_readlane(end, l) - __builtin_amdgcn_readlane(tiles, l));
       s.lo = __builtin_amdgcn_readlane((int)lo, l);
       s.hi = __builtin_amdgcn_readlane((int)hi, l);
       // (offsets that decrease may count more tiles than there are)
-      if (s.index < 0 || s.index >= s.count) s.g = -1;
+      if (s.index >= 0 && s.lo + (long long)s.index * len < s.hi) s.g = g0 + l;
       return s;
     }
     before = __builtin_amdgcn_readlane(end, 63);
   }
   return s;
+}
+
+// dw: the rows of the batch are cut into chunks of equal length, wherever the
+// groups end, so that every block has the same work; a block goes through the
+// groups that its chunk meets.  The chunks that hold rows of [lo, hi); a group
+// without rows belongs to the chunk that it lies in.
+__device__ __forceinline__ void chunks_of(const Groups& gr, int chunk, int chunks, long long lo, long long hi,
+                                          int& first, int& last) {
+  first = (int)(lo / chunk < chunks ? lo / chunk : chunks - 1);
+  last = hi > lo ? (int)((hi - 1) / chunk) : first;
 }
 
 // ---- operands -------------------------------------------------------------------
@@ -191,45 +191,82 @@ struct Stage {
     }
   }
 
-  // Four k of one row and the planes of their values.
-  __device__ __forceinline__ static void put4(uint16_t* lds, int at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  // FP32: four k of one row as planes, 5.5 instructions per value plus one that
+  // notices what they do not hold: where x - hi is not finite (x an infinity or
+  // NaN, or so large that hi rounded to infinity) `bad` becomes NaN.
+  __device__ __forceinline__ static void put4(uint16_t* lds, int at, const float* x, float& bad) {
+    typedef float f2_t __attribute__((ext_vector_type(2)));
+    typedef b16 b2_t __attribute__((ext_vector_type(2)));
+    uint32_t p[3][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float a = x[2 * h], b = x[2 * h + 1];
+#pragma unroll
+      for (int q = 0; q < 3; ++q) {
+        p[q][h] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f2_t{a, b}, b2_t));
+        if (q == 2) break;
+        a -= __uint_as_float(p[q][h] << 16);
+        b -= __uint_as_float(p[q][h] & 0xffff0000u);
+        if (q == 0) bad = __builtin_fmaf(b, 0.f, __builtin_fmaf(a, 0.f, bad));
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < 3; ++q) *(u2_t*)(lds + (size_t)q * R * BK + at) = u2_t{p[q][0], p[q][1]};
+  }
+  // The same for any value (split3).
+  __device__ static void put4_any(uint16_t* lds, int at, const float* x) {
     uint32_t p[4][3];
-    split3(__uint_as_float(a), p[0]);
-    split3(__uint_as_float(b), p[1]);
-    split3(__uint_as_float(c), p[2]);
-    split3(__uint_as_float(d), p[3]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) split3(x[i], p[i]);
 #pragma unroll
     for (int q = 0; q < 3; ++q)
       *(u2_t*)(lds + (size_t)q * R * BK + at) = u2_t{(p[0][q] >> 16) | p[1][q], (p[2][q] >> 16) | p[3][q]};
   }
 
   __device__ __forceinline__ void put(uint16_t* lds) const {
-    const int tid = threadIdx.x;
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const int u = i * TH + tid;
-      if (UNITS % TH != 0 && u >= UNITS) break;
+    for (int i = 0; i < U; ++i) put(lds, i);
+  }
+  __device__ __forceinline__ void put(uint16_t* lds, int i) const {
+    const int u = i * TH + threadIdx.x;
+    if (UNITS % TH == 0 || u < UNITS) {
       if constexpr (!TR) {
         const int at = lds_at<BK>(u / CH, u % CH);
         if constexpr (B) {
           *(u4_t*)(lds + at) = w[i][0];
         } else {
-          put4(lds, at, w[i][0][0], w[i][0][1], w[i][0][2], w[i][0][3]);
-          put4(lds, at + 4, w[i][1][0], w[i][1][1], w[i][1][2], w[i][1][3]);
+          float x[8], bad = 0.f;
+          __builtin_memcpy(x, w[i], 32);
+          put4(lds, at, x, bad);
+          put4(lds, at + 4, x + 4, bad);
+          if (bad != bad) {
+            put4_any(lds, at, x);
+            put4_any(lds, at + 4, x + 4);
+          }
         }
       } else {
         const int r = (u % (R / RU)) * RU, kg = u / (R / RU);
+        if constexpr (B) {
 #pragma unroll
-        for (int e = 0; e < RU; ++e) {
-          const int at = lds_at<BK>(r + e, kg >> 1) + 4 * (kg & 1);
-          if constexpr (B) {
+          for (int e = 0; e < RU; ++e) {
             uint32_t x[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) x[j] = w[i][j][e >> 1];
             const uint32_t sel = e & 1 ? 0x07060302u : 0x05040100u;     // the upper or lower halves of a pair
-            *(u2_t*)(lds + at) = u2_t{__builtin_amdgcn_perm(x[1], x[0], sel), __builtin_amdgcn_perm(x[3], x[2], sel)};
-          } else {
-            put4(lds, at, w[i][0][e], w[i][1][e], w[i][2][e], w[i][3][e]);
+            *(u2_t*)(lds + lds_at<BK>(r + e, kg >> 1) + 4 * (kg & 1)) =
+                u2_t{__builtin_amdgcn_perm(x[1], x[0], sel), __builtin_amdgcn_perm(x[3], x[2], sel)};
+          }
+        } else {
+          float x[4][4], bad = 0.f;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[e][j] = __uint_as_float(w[i][j][e]);
+            put4(lds, lds_at<BK>(r + e, kg >> 1) + 4 * (kg & 1), x[e], bad);
+          }
+          if (bad != bad) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) put4_any(lds, lds_at<BK>(r + e, kg >> 1) + 4 * (kg & 1), x[e]);
           }
         }
       }
@@ -251,10 +288,10 @@ struct Args {
   void* out;      long long ldo;     // y, dx, dw
   void* z;        long long ldz;     // FWD
   void* db;                          // DW
-  float* part;                       // DW: [slot][d_out][d_in] of groups with several chunks
-  float* part_b;                     // DW: [slot][d_out]
+  float* part;                       // DW: [chunk + group][d_out][d_in] of groups in several chunks
+  float* part_b;                     // DW: [chunk + group][d_out]
   int chunk;                         // DW: rows of a chunk
-  int tiles;                         // FWD, DX: row tiles (an upper bound); DW: chunks
+  int tiles;                         // FWD, DX: row tiles (an upper bound); DW: chunks (at least 1)
   int nt;                            // column tiles of a row tile; DW: tiles of dw
   int nt_in;                         // DW: tiles along d_in
   bool past, past_z;                 // whether out and z are stored past the caches
@@ -264,44 +301,69 @@ struct Args {
 // values of k.
 template <class T>
 struct Tile {
-  Span s;
-  int t;                      // row tile or chunk
   const T *a, *b;
   long long m0, m_end, n0, n_end, nk;
+  int g;                      // group
+  int slot;                   // DW: where its part goes, -1: the group is whole
 };
 
-template <class T, int BM, int BN, int MODE>
-__device__ __forceinline__ bool locate(const Args& g, Tile<T>& w) {
+// Calls `work` for the block's tile, or for each of its chunk's groups (DW).
+template <class T, int BM, int BN, int MODE, class Work>
+__device__ __forceinline__ void each_tile(const Args& g, Work&& work) {
   // Many row tiles: the column tiles of one on one XCD, next to each other, so
   // that its rows are read from that L2.  Few: all tiles over all XCDs.  (DW:
-  // the tiles of one chunk; its rows are most of what the pass reads.)
-  const bool many = g.tiles >= (MODE == DW ? 8 : 64);
+  // the tiles of one chunk, whose rows are most of what the pass reads.)
+  const bool many = MODE == DW ? g.tiles % 8 == 0 : g.tiles >= 64;
   const int lin = many ? blockIdx.x >> 3 : blockIdx.x;
   const int c = lin % g.nt;
-  w.t = many ? (lin / g.nt) * 8 + (blockIdx.x & 7) : lin / g.nt;
-  if (w.t >= g.tiles) return false;
-  w.s = find_tile(g.gr, w.t, MODE == DW ? g.chunk : BM, MODE == DW ? 1 : 0);
-  if (w.s.g < 0) return false;
-  w.a = (const T*)g.a;
-  w.b = (const T*)g.b;
+  const int t = many ? (lin / g.nt) * 8 + (blockIdx.x & 7) : lin / g.nt;
+  if (t >= g.tiles) return;
+  Tile<T> w;
   if constexpr (MODE == DW) {
-    const long long lo = w.s.lo + (long long)w.s.index * g.chunk;
-    w.nk = w.s.hi - lo < g.chunk ? w.s.hi - lo : g.chunk;
-    w.a += lo * g.lda;
-    w.b += lo * g.ldb;
+    const int lane = threadIdx.x & 63, groups = g.gr.n ? g.gr.n : 1;
+    const long long begin = (long long)t * g.chunk, end = begin + g.chunk;
     w.m0 = (long long)(c / g.nt_in) * BM;
     w.n0 = (long long)(c % g.nt_in) * BN;
     w.m_end = g.d_out;
     w.n_end = g.d_in;
+    for (int g0 = 0; g0 < groups; g0 += 64) {
+      long long lo = 0, hi = g.gr.rows;
+      int first = 0, last = -1;
+      if (g0 + lane < groups) {
+        if (g.gr.n) group_rows(g.gr, g0 + lane, lo, hi);
+        chunks_of(g.gr, g.chunk, g.tiles, lo, hi, first, last);
+      }
+      for (unsigned long long todo = __ballot(first <= t && t <= last); todo; todo &= todo - 1) {
+        const int l = __ffsll((long long)todo) - 1;
+        const bool whole = __builtin_amdgcn_readlane(first, l) == __builtin_amdgcn_readlane(last, l);
+        long long r0 = begin, r1 = end < g.gr.rows ? end : g.gr.rows;
+        if (g.gr.n) {
+          const long long glo = __builtin_amdgcn_readlane((int)lo, l), ghi = __builtin_amdgcn_readlane((int)hi, l);
+          r0 = glo > r0 ? glo : r0;
+          r1 = ghi < r1 ? ghi : r1;
+        }
+        w.g = g0 + l;
+        w.slot = whole ? -1 : t + w.g;
+        w.nk = r1 > r0 ? r1 - r0 : 0;
+        w.a = (const T*)g.a + r0 * g.lda;
+        w.b = (const T*)g.b + r0 * g.ldb;
+        work(w);
+      }
+    }
   } else {
-    w.m0 = w.s.lo + (long long)w.s.index * BM;
-    w.m_end = w.s.hi;
+    const Span s = find_tile(g.gr, t, BM);
+    if (s.g < 0) return;
+    w.g = s.g;
+    w.slot = -1;
+    w.a = (const T*)g.a;
+    w.b = (const T*)g.b + (size_t)s.g * g.d_out * g.d_in;
+    w.m0 = s.lo + (long long)s.index * BM;
+    w.m_end = s.hi;
     w.n0 = (long long)c * BN;
     w.n_end = MODE == FWD ? g.d_out : g.d_in;
     w.nk = MODE == FWD ? g.d_in : g.d_out;
-    w.b += (size_t)w.s.g * g.d_out * g.d_in;
+    work(w);
   }
-  return true;
 }
 
 // The tile's results.  A lane holds, per fragment, row l % 16 and the columns
@@ -320,19 +382,20 @@ __device__ __forceinline__ void finish(const Args& g, const Tile<T>& w, int wm, 
   float* my = lds + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * finish_floats<FN>();
   const size_t wsize = (size_t)g.d_out * g.d_in;
   const long long n = w.n0 + wn + (lane % LPR) * 8, left = w.n_end - n;
-  const bool whole = MODE != DW || w.s.count == 1;
-  T* out = (T*)g.out + (MODE == DW ? (size_t)w.s.g * wsize : 0) + n;
-  float* part = MODE == DW && !whole ? g.part + (size_t)w.t * wsize + n : nullptr;
+  const bool whole = MODE != DW || w.slot < 0;
+  T* out = (T*)g.out + (MODE == DW ? (size_t)w.g * wsize : 0) + n;
+  float* part = MODE == DW && !whole ? g.part + (size_t)w.slot * wsize + n : nullptr;
   const long long ldo = MODE == DW ? g.d_in : g.ldo;
   float bias[8];
-  if (MODE == FWD && g.bias) load_n<8>((const T*)g.bias + (size_t)w.s.g * g.d_out + n, left, bias);
+  if (MODE == FWD && g.bias) load_n<8>((const T*)g.bias + (size_t)w.g * g.d_out + n, left, bias);
+  constexpr int PASSES = (16 + RPP - 1) / RPP;
 #pragma unroll
   for (int i = 0; i < FM; ++i) {
 #pragma unroll
     for (int j = 0; j < FN; ++j) *(f4_t*)(my + lr * PITCH + 16 * j + 4 * lq) = acc[i][j];
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int q = 0; q < (16 + RPP - 1) / RPP; ++q) {
+    for (int q = 0; q < PASSES; ++q) {
       const int r = q * RPP + lane / LPR;
       const long long m = w.m0 + wm + 16 * i + r;
       if (lane < LPR * RPP && r < 16 && m < w.m_end && left > 0) {
@@ -379,24 +442,22 @@ __device__ __forceinline__ void finish(const Args& g, const Tile<T>& w, int wm, 
       const long long m = w.m0 + wm + 16 * i + lr;
       if (sum_b && lq == 0 && m < w.m_end) {
         const float v = accb[i][0];
-        if (whole) store<1>((T*)g.db + (size_t)w.s.g * g.d_out + m, &v);
-        else g.part_b[(size_t)w.t * g.d_out + m] = v;
+        if (whole) store<1>((T*)g.db + (size_t)w.g * g.d_out + m, &v);
+        else g.part_b[(size_t)w.slot * g.d_out + m] = v;
       }
     }
   }
 }
 
+template <class T, int BM, int BN>
+constexpr int stage_halfs() { return Mma<T>::NP * (BM + BN) * Mma<T>::BK; }
+
 template <class T, int BM, int BN, int WM, int WN, int MODE>
-__global__ void __launch_bounds__(64 * WM * WN, 2) k_dense(Args g) {
+__device__ __forceinline__ void product(const Args& g, const Tile<T>& w, uint16_t* lds) {
   using M = Mma<T>;
   constexpr int NP = M::NP, BK = M::BK, TH = 64 * WM * WN;
   constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
-  constexpr int SA = NP * BM * BK, SB = NP * BN * BK;
-  static_assert((SA + SB) * 2 >= WM * WN * finish_floats<FN>() * 4, "room for finish");
-  __shared__ __attribute__((aligned(16))) uint16_t As[SA + SB];
-  uint16_t* Bs = As + SA;
-  Tile<T> w;
-  if (!locate<T, BM, BN, MODE>(g, w)) return;
+  uint16_t *As = lds, *Bs = lds + NP * BM * BK;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, lr = lane & 15, lq = lane >> 4;
   const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
   const bool sum_b = MODE == DW && g.db != nullptr && w.n0 == 0 && wn == 0;
@@ -429,41 +490,49 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_dense(Args g) {
     }
 #pragma unroll
     for (int kk = 0; kk < BK / 32; ++kk) {
-      bf8_t fa[FM][NP], fb[FN][NP];
-#pragma unroll
-      for (int i = 0; i < FM; ++i)
-#pragma unroll
-        for (int p = 0; p < NP; ++p)
-          fa[i][p] = *(const bf8_t*)(As + p * BM * BK + lds_at<BK>(wm + 16 * i + lr, 4 * kk + lq));
+      bf8_t fb[FN][NP];
 #pragma unroll
       for (int j = 0; j < FN; ++j)
 #pragma unroll
         for (int p = 0; p < NP; ++p)
           fb[j][p] = *(const bf8_t*)(Bs + p * BN * BK + lds_at<BK>(wn + 16 * j + lr, 4 * kk + lq));
-      // smallest products first: lo hi, mid mid, hi lo, mid hi, hi mid, hi hi
-      constexpr int pa[6] = {2, 1, 0, 1, 0, 0}, pb[6] = {0, 1, 2, 0, 1, 0};
 #pragma unroll
-      for (int q = 0; q < M::NSUB; ++q) {
-        const int qa = NP == 1 ? 0 : pa[q], qb = NP == 1 ? 0 : pb[q];
+      for (int i = 0; i < FM; ++i) {
+        bf8_t fa[NP];
 #pragma unroll
-        for (int i = 0; i < FM; ++i)
+        for (int p = 0; p < NP; ++p)
+          fa[p] = *(const bf8_t*)(As + p * BM * BK + lds_at<BK>(wm + 16 * i + lr, 4 * kk + lq));
+        // smallest products first: lo hi, mid mid, hi lo, mid hi, hi mid, hi hi
+        constexpr int pa[6] = {2, 1, 0, 1, 0, 0}, pb[6] = {0, 1, 2, 0, 1, 0};
+#pragma unroll
+        for (int q = 0; q < M::NSUB; ++q)
 #pragma unroll
           for (int j = 0; j < FN; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j][qb], fa[i][qa], acc[i][j], 0, 0, 0);
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j][NP == 1 ? 0 : pb[q]], fa[NP == 1 ? 0 : pa[q]],
+                                                               acc[i][j], 0, 0, 0);
+        if constexpr (MODE == DW)
+          if (sum_b) {
+            // the column sums of dz, as a product with ones
+#pragma unroll
+            for (int p = NP - 1; p >= 0; --p)
+              accb[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, fa[p], accb[i], 0, 0, 0);
+          }
       }
-      if constexpr (MODE == DW)
-        if (sum_b) {
-          // the column sums of dz, as a product with ones
-#pragma unroll
-          for (int p = NP - 1; p >= 0; --p)
-#pragma unroll
-            for (int i = 0; i < FM; ++i)
-              accb[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, fa[i][p], accb[i], 0, 0, 0);
-        }
     }
     __syncthreads();
   }
-  finish<T, FM, FN, MODE>(g, w, wm, wn, acc, accb, sum_b, (float*)As);
+  finish<T, FM, FN, MODE>(g, w, wm, wn, acc, accb, sum_b, (float*)lds);
+}
+
+template <class T, int BM, int BN, int WM, int WN, int MODE>
+__global__ void __launch_bounds__(64 * WM * WN, 2) k_dense(Args g) {
+  constexpr int HALFS = stage_halfs<T, BM, BN>();
+  static_assert(HALFS * 2 >= WM * WN * finish_floats<BN / WN / 16>() * 4, "room for finish");
+  __shared__ __attribute__((aligned(16))) uint16_t lds[HALFS];
+  each_tile<T, BM, BN, MODE>(g, [&](const Tile<T>& w) {
+    product<T, BM, BN, WM, WN, MODE>(g, w, lds);
+    if constexpr (MODE == DW) __syncthreads();      // the next group's operands take its place
+  });
 }
 
 // ---- BF16 operands in 16-byte words -------------------------------------------------
@@ -562,16 +631,11 @@ struct Dma {
 };
 
 template <int BM, int BN, int WM, int WN, int MODE>
-__global__ void __launch_bounds__(64 * WM * WN, 2) k_dense16(Args g) {
-  constexpr int TH = 64 * WM * WN, BK = 64, NB = 2;
+__device__ __forceinline__ void product16(const Args& g, const Tile<b16>& w, uint16_t* lds) {
+  constexpr int TH = 64 * WM * WN, BK = 64, SA = BM * BK, S = SA + BN * BK;
   constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
   using A = Dma<BM, BK, TH, MODE == DW>;
   using B = Dma<BN, BK, TH, MODE != FWD>;
-  constexpr int SA = BM * BK, SB = BN * BK;
-  static_assert(NB * (SA + SB) * 2 >= WM * WN * finish_floats<FN>() * 4, "room for finish");
-  __shared__ __attribute__((aligned(16))) uint16_t lds[NB][SA + SB];
-  Tile<b16> w;
-  if (!locate<b16, BM, BN, MODE>(g, w)) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
   const bool sum_b = MODE == DW && g.db != nullptr && w.n0 == 0 && wn == 0;
@@ -593,8 +657,8 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_dense16(Args g) {
   sb.init(w.b, g.ldb, w.n0, w.n_end);
   long long left = w.nk;                // k from the block being read on
   auto fetch = [&](int buf, long long from) {
-    sa.next(lds[buf], g.lda, from);
-    sb.next(lds[buf] + SA, g.ldb, from);
+    sa.next(lds + buf * S, g.lda, from);
+    sb.next(lds + buf * S + SA, g.ldb, from);
   };
   if (left > 0) fetch(0, left);
   for (int cur = 0; left > 0; cur ^= 1, left -= BK) {
@@ -602,7 +666,7 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_dense16(Args g) {
     wait_loads();
     __syncthreads();
     if (left > BK) fetch(cur ^ 1, left - BK);
-    const uint16_t *a = lds[cur], *b = a + SA;
+    const uint16_t *a = lds + cur * S, *b = a + SA;
     bf8_t fa[2][FM], fb[2][FN];
     auto read = [&](int kk) {
 #pragma unroll
@@ -644,6 +708,96 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_dense16(Args g) {
   finish<b16, FM, FN, MODE>(g, w, wm, wn, acc, accb, sum_b, (float*)lds);
 }
 
+template <int BM, int BN, int WM, int WN, int MODE>
+__global__ void __launch_bounds__(64 * WM * WN, 2) k_dense16(Args g) {
+  constexpr int HALFS = 2 * (BM + BN) * 64;
+  static_assert(HALFS * 2 >= WM * WN * finish_floats<BN / WN / 16>() * 4, "room for finish");
+  __shared__ __attribute__((aligned(16))) uint16_t lds[HALFS];
+  each_tile<b16, BM, BN, MODE>(g, [&](const Tile<b16>& w) {
+    product16<BM, BN, WM, WN, MODE>(g, w, lds);
+    if constexpr (MODE == DW) __syncthreads();      // the next group's operands take its place
+  });
+}
+
+// ---- few rows ---------------------------------------------------------------------
+// The forward of a few rows reads its weights once and little else: a block has
+// 16 rows x 16 columns, its four waves share out k and load their fragments
+// from memory straight into registers, all of a wave's loads of 128 k at once;
+// their sums meet in LDS.
+template <class T>
+struct Words8 {                     // 8 k of one row: 16 or 32 bytes
+  float x[8];
+  __device__ __forceinline__ void planes(bf8_t* f) const {
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[0][i] = (b16)x[i];      // (exact)
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        uint32_t p[3];
+        split3(x[i], p);
+#pragma unroll
+        for (int q = 0; q < 3; ++q) f[q][i] = __builtin_bit_cast(b16, (uint16_t)(p[q] >> 16));
+      }
+    }
+  }
+};
+
+template <class T>
+__global__ void __launch_bounds__(256) k_few(Args g) {
+  using M = Mma<T>;
+  constexpr int NP = M::NP, AHEAD = 4;
+  __shared__ f4_t sums[4][64];
+  each_tile<T, 16, 16, FWD>(g, [&](const Tile<T>& w) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int lr = lane & 15, lq = lane >> 4;
+    const long long m = w.m0 + lr, n = w.n0 + lr;
+    const T* pa = w.a + (m < w.m_end ? m : w.m_end - 1) * g.lda;
+    const T* pb = w.b + (n < w.n_end ? n : w.n_end - 1) * g.ldb;
+    f4_t acc = {0, 0, 0, 0};
+    for (long long k0 = 32 * wave; k0 < w.nk; k0 += 128 * AHEAD) {
+      Words8<T> a[AHEAD], b[AHEAD];
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {
+        const long long k = k0 + 128 * i + 8 * lq;
+        load_n<8>(pa + k, w.nk - k, a[i].x);
+        load_n<8>(pb + k, w.nk - k, b[i].x);
+      }
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {
+        bf8_t fa[NP], fb[NP];
+        a[i].planes(fa);
+        b[i].planes(fb);
+        constexpr int pa6[6] = {2, 1, 0, 1, 0, 0}, pb6[6] = {0, 1, 2, 0, 1, 0};
+#pragma unroll
+        for (int q = 0; q < M::NSUB; ++q)
+          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[NP == 1 ? 0 : pb6[q]], fa[NP == 1 ? 0 : pa6[q]], acc, 0, 0, 0);
+      }
+    }
+    sums[wave][lane] = acc;
+    __syncthreads();
+    const long long c = w.n0 + 4 * lq, left = w.n_end - c;
+    if (wave == 0 && m < w.m_end && left > 0) {
+      float v[4], e[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) v[r] = (acc[r] + sums[1][lane][r]) + (sums[2][lane][r] + sums[3][lane][r]);
+      if (g.bias) {
+        load_n<4>((const T*)g.bias + (size_t)w.g * g.d_out + c, left, e);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] += e[r];
+      }
+      if (g.z) store_n<4>((T*)g.z + m * g.ldz + c, left, v);
+      act<4>(v, g.act);
+      if (g.e) {
+        load_n<4>((const T*)g.e + m * g.lde + c, left, e);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] += e[r];
+      }
+      store_n<4>((T*)g.out + m * g.ldo + c, left, v);
+    }
+  });
+}
+
 // dz = dy activation'(z), [rows][d_out] without gaps.
 template <class T>
 __global__ void __launch_bounds__(256) k_dz(long long rows, int d_out, const T* __restrict__ dy, long long lddy,
@@ -661,29 +815,18 @@ __global__ void __launch_bounds__(256) k_dz(long long rows, int d_out, const T* 
   store_n<V>(dz + r * d_out + c, d_out - c, d);
 }
 
-// dw and dbias of the groups that have several chunks: their parts added in
+// dw and dbias of the groups that lie in several chunks: their parts added in
 // the order of the rows.  blockIdx.y: the group.
 template <class T>
 __global__ void __launch_bounds__(256) k_fold(Args g) {
-  const int grp = blockIdx.y, lane = threadIdx.x & 63;
-  // the group's first chunk, by the same count as find_tile's
-  int first = 0, count = 0;
-  if (g.gr.n == 0) {
-    count = (int)((g.gr.rows + g.chunk - 1) / g.chunk);
-  } else {
-    long long lo, hi;
-    for (int k = lane; k < grp; k += 64) {
-      group_rows(g.gr, k, lo, hi);
-      const int n = (int)((hi - lo + g.chunk - 1) / g.chunk);
-      first += n < 1 ? 1 : n;
-    }
-#pragma unroll
-    for (int o = 32; o; o >>= 1) first += __shfl_xor(first, o);
-    group_rows(g.gr, grp, lo, hi);
-    count = (int)((hi - lo + g.chunk - 1) / g.chunk);
-  }
-  if (count > g.tiles - first) count = g.tiles - first;   // (offsets that decrease)
-  if (first < 0 || count <= 1) return;
+  const int grp = blockIdx.y;
+  long long lo = 0, hi = g.gr.rows;
+  if (g.gr.n) group_rows(g.gr, grp, lo, hi);
+  int first, last;
+  chunks_of(g.gr, g.chunk, g.tiles, lo, hi, first, last);
+  const int count = last - first + 1;
+  if (count == 1) return;
+  first += grp;
   const size_t wsize = (size_t)g.d_out * g.d_in;
   const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
   if (i < wsize) {
@@ -707,14 +850,20 @@ __global__ void __launch_bounds__(256) k_fold(Args g) {
 inline long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 
 // Upper bound of the row tiles of `len` rows.
-inline long long tile_bound(const Groups& gr, int len, int least) {
-  const long long n = ceil_div(gr.rows, len);
-  return gr.n ? n + gr.n : n < least ? least : n;
-}
+inline long long tile_bound(const Groups& gr, int len) { return ceil_div(gr.rows, len) + gr.n; }
+
+// Blocks that fill the card: 256 CUs, two blocks each.
+constexpr long long FULL = 512;
 
 // Whether an operand's rows can be read in 16-byte words.
 inline bool words(const void* p, long long ld, int width) {
   return (uintptr_t)p % 16 == 0 && ld % 8 == 0 && ld < (1 << 22) && width % 8 == 0;
+}
+
+template <int MODE>
+bool words_path(const Args& a) {
+  return words(a.a, a.lda, MODE == FWD ? a.d_in : a.d_out) && words(a.b, a.ldb, a.d_in) &&
+         (size_t)a.d_out * a.d_in % 8 == 0;
 }
 
 // Whether an output is stored past the caches: where it is larger than the
@@ -729,34 +878,91 @@ inline bool past_caches(const void* p, long long ld, long long rows, size_t es) 
 template <class T, int BM, int BN, int WM, int WN, int MODE>
 bool launch(hipStream_t st, Args a, long long tiles, long long nt) {
   if (tiles > 0x7fffffffLL / (nt < 8 ? 8 : nt) - 8) return false;
-  const long long blocks = (tiles >= (MODE == DW ? 8 : 64) ? ceil_div(tiles, 8) * 8 : tiles) * nt;
+  const long long blocks = (MODE != DW && tiles >= 64 ? ceil_div(tiles, 8) * 8 : tiles) * nt;
   if (blocks == 0) return true;
   a.tiles = (int)tiles;
   a.nt = (int)nt;
   a.past = past_caches(a.out, a.ldo, a.gr.rows, sizeof(T));
   a.past_z = past_caches(a.z, a.ldz, a.gr.rows, sizeof(T));
   if constexpr (sizeof(T) == 2) {
-    if (words(a.a, a.lda, MODE == FWD ? a.d_in : a.d_out) && words(a.b, a.ldb, a.d_in) &&
-        (size_t)a.d_out * a.d_in % 8 == 0) {
+    if (words_path<MODE>(a)) {
       k_dense16<BM, BN, WM, WN, MODE><<<dim3((unsigned)blocks), 64 * WM * WN, 0, st>>>(a);
       return true;
     }
   }
-  k_dense<T, BM, BN, WM, WN, MODE><<<dim3((unsigned)blocks), 64 * WM * WN, 0, st>>>(a);
+  if constexpr (BM > 128 || BN > 128) return false;
+  else k_dense<T, BM, BN, WM, WN, MODE><<<dim3((unsigned)blocks), 64 * WM * WN, 0, st>>>(a);
   return true;
 }
 
-// Blocks that fill the card: 256 CUs, two blocks each.
-constexpr long long FULL = 512;
+// Rounds of tiles of bm x bn that a card with `at_once` of them in work goes
+// through (a group's last tile is half empty on average).
+inline long long rounds(const Groups& gr, int bm, int width, int bn, long long at_once) {
+  return ceil_div((ceil_div(gr.rows, bm) + gr.n / 2) * ceil_div(width, bn), at_once);
+}
 
-// FWD and DX: tiles of 128 x 128, or of 64 x 64 where those leave CUs idle.
+// FWD and DX: tiles of 128 x 128, two to a CU, or of 64 x 64 where those leave
+// CUs idle.  BF16 words: the tiles of least cost, where a round of 128 x 128
+// counts 1, of 128 x 160 (for widths like 776 = 4.85 x 160) 1.25 and of 256 x
+// 256, one to a CU, 1.74: it moves half the bytes per product through the
+// caches.  us at 65,500 rows for 128 x 128 / 128 x 160 / 256 x 256 with the
+// costs in brackets: 776 -> 776 134 / 119 / 131 (7 / 6.3 / 7); 1,024 -> 1,024
+// 159 / 171 / 143 (8 / 8.8 / 7); 256 -> 1,024 63 / 67 / 55 (8 / 8.8 / 7); 1,024
+// -> 256 45 / 50 / 40 (2 / 2.5 / 1.7); 256 -> 384, z kept, 33 / 46 / 37 (3 /
+// 3.8 / 3.5).
 template <class T, int MODE>
 bool run_rows(hipStream_t st, const Args& a) {
   const int width = MODE == FWD ? a.d_out : a.d_in;
-  const long long big = tile_bound(a.gr, 128, 0) * ceil_div(width, 128);
-  if (big >= FULL / 2)
-    return launch<T, 128, 128, 2, 2, MODE>(st, a, tile_bound(a.gr, 128, 0), ceil_div(width, 128));
-  return launch<T, 64, 64, 2, 2, MODE>(st, a, tile_bound(a.gr, 64, 0), ceil_div(width, 64));
+  const long long rows = tile_bound(a.gr, 128), cols = ceil_div(width, 128);
+  if constexpr (MODE == FWD) {
+    // (up to 128 rows of 776: 7.9 to 8.5 us against 10.6 in tiles of 64 x 64,
+    // FP32 13 to 18 against 36; at 512 rows 14.6 against 10.9, 39 against 37)
+    if (tile_bound(a.gr, 16) * ceil_div(width, 16) <= FULL) {
+      Args b = a;
+      b.tiles = (int)tile_bound(a.gr, 16);
+      b.nt = (int)ceil_div(width, 16);
+      const long long blocks = (b.tiles >= 64 ? ceil_div(b.tiles, 8) * 8 : b.tiles) * (long long)b.nt;
+      k_few<T><<<dim3((unsigned)blocks), 256, 0, st>>>(b);
+      return true;
+    }
+  }
+  if (rows * cols < FULL / 2)
+    return launch<T, 64, 64, 2, 2, MODE>(st, a, tile_bound(a.gr, 64), ceil_div(width, 64));
+  if constexpr (sizeof(T) == 2) {
+    if (words_path<MODE>(a)) {
+      const double c128 = (double)rounds(a.gr, 128, width, 128, FULL);
+      const double c160 = 1.25 * rounds(a.gr, 128, width, 160, FULL);
+      const double c256 = 1.74 * rounds(a.gr, 256, width, 256, FULL / 2);
+      if (c256 < c128 && c256 < c160)
+        return launch<T, 256, 256, 2, 4, MODE>(st, a, tile_bound(a.gr, 256), ceil_div(width, 256));
+      if (c160 < c128) return launch<T, 128, 160, 2, 2, MODE>(st, a, rows, ceil_div(width, 160));
+    }
+  }
+  return launch<T, 128, 128, 2, 2, MODE>(st, a, rows, cols);
+}
+
+// Chunks of the rows for dw, nt tiles each.  More of them fill the card
+// better, and each adds a part of dw to be written and read: a k-block takes
+// a block about `step` us (two blocks to a CU), a part 0.033 us per tile.  A
+// multiple of 8 in BF16: a chunk's tiles on one XCD read its rows from one L2
+// (776 -> 776, 65,502 rows: 264 us with 10 chunks over all XCDs, 132 with 8).
+inline long long dw_chunks(long long rows, long long nt, int groups, bool half) {
+  const int block_k = half ? 64 : 32;
+  const double step = half ? 1.0 : 1.5;
+  const long long most = rows / 64 < 512 ? rows / 64 : 512;
+  const int by = half && most >= 8 ? 8 : 1;
+  long long best = 1;
+  double least = 1e300;
+  for (long long s = by; s <= (most > by ? most : by); s += by) {
+    const double t = (double)ceil_div(s * nt, FULL) * rows / s / block_k * step + 0.033 * s * nt;
+    if (t < least) {
+      least = t;
+      best = s;
+    }
+  }
+  // (a block goes through its chunk's groups one by one)
+  while (best * 4 < groups && best * 64 < rows) best *= 2;
+  return best;
 }
 
 template <class T>
@@ -785,21 +991,19 @@ painn_status run_bwd(painn_ctx* ctx, const painn_linear_backward_args& p, int n_
   a.gr = Groups{n_groups, offsets, p.rows};
   a.d_in = p.d_in; a.d_out = p.d_out;
   a.a = p.dy; a.lda = p.lddy;
-  // dw: chunks of rows so that its tiles fill the card
   const size_t wsize = (size_t)p.d_out * p.d_in;
   const bool big = p.d_in > 64 && p.d_out > 64;
   const int bt = big ? 128 : 64;
   const long long nt = ceil_div(p.d_out, bt) * ceil_div(p.d_in, bt);
-  const long long fit = FULL / nt > 1 ? FULL / nt : 1, want = fit < 8 ? fit : fit / 8 * 8;   // (8 XCDs)
-  const long long chunk = ((ceil_div(p.rows, want) + 255) / 256) * 256;
-  a.chunk = (int)(chunk < 256 ? 256 : chunk > (1 << 24) ? 1 << 24 : chunk);
-  const long long slots = tile_bound(a.gr, a.chunk, 1);
+  const long long cut = ceil_div(p.rows, dw_chunks(p.rows, nt, n_groups, sizeof(T) == 2));
+  a.chunk = (int)(cut < 1 ? 1 : cut > (1 << 30) ? 1 << 30 : cut);
+  const long long chunks = p.rows > 0 ? ceil_div(p.rows, a.chunk) : 1;
   const bool have_dz = p.activation != PAINN_ACT_NONE && p.rows > 0;
   const size_t dz_bytes = have_dz ? align256((size_t)p.rows * p.d_out * sizeof(T)) : 0;
-  // (one chunk per group: no parts)
-  const bool parts = p.dw && ceil_div(p.rows, a.chunk) > 1;
-  const size_t part_bytes = parts ? align256((size_t)slots * wsize * sizeof(float)) : 0;
-  const size_t need = dz_bytes + part_bytes + (parts ? (size_t)slots * p.d_out * sizeof(float) : 0);
+  const bool parts = p.dw && chunks > 1;
+  const size_t slots = (size_t)(chunks + G - 1);
+  const size_t part_bytes = parts ? align256(slots * wsize * sizeof(float)) : 0;
+  const size_t need = dz_bytes + part_bytes + (parts ? slots * p.d_out * sizeof(float) : 0);
   if (need) {
     const painn_status st = ops_workspace(ctx, need);
     if (st != PAINN_OK) return st;
@@ -825,8 +1029,8 @@ painn_status run_bwd(painn_ctx* ctx, const painn_linear_backward_args& p, int n_
     d.part = (float*)(ws + dz_bytes);
     d.part_b = (float*)(ws + dz_bytes + part_bytes);
     d.nt_in = (int)ceil_div(p.d_in, bt);
-    d.tiles = (int)slots;
-    ok = big ? launch<T, 128, 128, 2, 2, DW>(st, d, slots, nt) : launch<T, 64, 64, 2, 2, DW>(st, d, slots, nt);
+    d.tiles = (int)chunks;
+    ok = big ? launch<T, 128, 128, 2, 2, DW>(st, d, chunks, nt) : launch<T, 64, 64, 2, 2, DW>(st, d, chunks, nt);
     if (ok && parts) k_fold<T><<<dim3((unsigned)ceil_div(wsize, 1024), G), 256, 0, st>>>(d);
   }
   if (ok && p.dx && p.rows > 0) {

@@ -180,6 +180,7 @@ class Runtime:
         self.device = torch.device("cuda", device)
         self.stream = torch.cuda.current_stream(self.device)
         self.ctx = B.painn_create(device, self.stream.cuda_stream)
+        self._stream_id = self.stream.cuda_stream
 
     # ---- inputs ----------------------------------------------------------
     def upload_batch(self, batch):
@@ -292,9 +293,9 @@ class Runtime:
     # sees the order of its own stream.
     def _enter(self):
         import torch
-        cur = torch.cuda.current_stream(self.device)
-        if cur == self.stream:
+        if torch._C._cuda_getCurrentRawStream(self.device.index) == self._stream_id:
             return None
+        cur = torch.cuda.current_stream(self.device)
         self.stream.wait_stream(cur)
         return cur
 
@@ -312,71 +313,74 @@ class Runtime:
         except KeyError:
             raise ValueError(f"the operators take float32 or bfloat16, not {x.dtype}") from None
 
-    def _rows(self, t, name, like, rows, cols):
-        """(pointer, row stride) of a matrix whose rows are contiguous."""
+    def _rows(self, t, name, dtype, rows, cols):
+        """(pointer, row stride) of a matrix whose rows are contiguous; (0, 0)
+        for None."""
         if t is None:
-            return None, 0
-        if t.dtype != like.dtype or t.device != self.device:
-            raise ValueError(f"{name} must be {like.dtype} on {self.device}, not {t.dtype} on {t.device}")
-        if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+            return 0, 0
+        if t.dtype is not dtype or t.device != self.device:
+            raise ValueError(f"{name} must be {dtype} on {self.device}, not {t.dtype} on {t.device}")
+        if t.shape != (rows, cols):
             raise ValueError(f"{name} must be [{rows}, {cols}], not {list(t.shape)}")
-        ld = t.stride(0)
-        if rows <= 1 or cols == 0:
-            ld = max(ld, cols)
-        if (cols > 1 and t.stride(1) != 1) or ld < cols:
+        ld, step = t.stride()
+        if rows <= 1 and ld < cols:
+            ld = cols
+        if (step != 1 and cols > 1) or ld < cols:
             raise ValueError(f"{name} must have contiguous rows that do not overlap (strides {t.stride()})")
-        return t.data_ptr() or None, ld
+        return t.data_ptr(), ld
 
     def _whole(self, t, name, dtype, shape):
-        """Pointer of a contiguous tensor."""
+        """Pointer of a contiguous tensor; 0 for None."""
         if t is None:
-            return None
-        if t.dtype != dtype or t.device != self.device or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+            return 0
+        if t.dtype is not dtype or t.device != self.device or t.shape != shape or not t.is_contiguous():
             raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {list(shape)} on {self.device}, "
                              f"not {t.dtype} {list(t.shape)} on {t.device}")
-        return t.data_ptr() or None
+        return t.data_ptr()
 
     def layer_norm(self, x, weight, bias, eps=1e-5, out=None):
         """(y, mean, rstd) of every row of x [rows, cols]; mean and rstd [rows]
         are FP32 and go to layer_norm_backward.  `out` may be x."""
         import torch
-        prec = self._precision(x)
+        prec, t = self._precision(x), x.dtype
         if x.dim() != 2:
             raise ValueError("x must be [rows, cols]")
         n, c = x.shape
-        px, ldx = self._rows(x, "x", x, n, c)
-        pw, pb = self._whole(weight, "weight", x.dtype, (c,)), self._whole(bias, "bias", x.dtype, (c,))
+        px, ldx = self._rows(x, "x", t, n, c)
+        pw, pb = self._whole(weight, "weight", t, (c,)), self._whole(bias, "bias", t, (c,))
         if out is None:
-            out = torch.empty((n, c), dtype=x.dtype, device=self.device)
-        py, ldy = self._rows(out, "out", x, n, c)
-        stats = torch.empty((2, n), dtype=torch.float32, device=self.device)
-        ps = stats.data_ptr()
+            out = x.new_empty((n, c))
+        py, ldy = self._rows(out, "out", t, n, c)
+        stats = x.new_empty((2, n), dtype=torch.float32)
+        mean, rstd = stats.unbind()
         cur = self._enter()
-        B.painn_layer_norm(self.ctx, prec, n, c, px, ldx, pw, pb, eps, py, ldy, ps or None, ps + 4 * n or None)
-        self._leave(cur, (x, weight, bias, out, stats))
-        return out, stats[0], stats[1]
+        B.painn_layer_norm(self.ctx, prec, n, c, px, ldx, pw, pb, eps, py, ldy, mean.data_ptr(), rstd.data_ptr())
+        if cur is not None:
+            self._leave(cur, (x, weight, bias, out, stats))
+        return out, mean, rstd
 
     def layer_norm_backward(self, dy, x, weight, mean, rstd, dx=None, dweight=None, dbias=None, need_dx=True):
         """(dx, dweight, dbias) from dy and the forward's x, mean and rstd; dx
         is None without need_dx and may be given as dy."""
         import torch
-        prec = self._precision(x)
+        prec, t = self._precision(x), x.dtype
         if x.dim() != 2:
             raise ValueError("x must be [rows, cols]")
         n, c = x.shape
-        px, ldx = self._rows(x, "x", x, n, c)
-        pd, ldd = self._rows(dy, "dy", x, n, c)
-        pw = self._whole(weight, "weight", x.dtype, (c,))
-        pm, pr = (self._whole(t, k, torch.float32, (n,)) for t, k in ((mean, "mean"), (rstd, "rstd")))
+        px, ldx = self._rows(x, "x", t, n, c)
+        pd, ldd = self._rows(dy, "dy", t, n, c)
+        pw = self._whole(weight, "weight", t, (c,))
+        pm, pr = (self._whole(a, k, torch.float32, (n,)) for a, k in ((mean, "mean"), (rstd, "rstd")))
         if need_dx and dx is None:
-            dx = torch.empty((n, c), dtype=x.dtype, device=self.device)
+            dx = x.new_empty((n, c))
         dweight = torch.empty_like(weight) if dweight is None else dweight
         dbias = torch.empty_like(weight) if dbias is None else dbias
-        po, ldo = self._rows(dx, "dx", x, n, c)
-        pg, pb = self._whole(dweight, "dweight", x.dtype, (c,)), self._whole(dbias, "dbias", x.dtype, (c,))
+        po, ldo = self._rows(dx, "dx", t, n, c)
+        pg, pb = self._whole(dweight, "dweight", t, (c,)), self._whole(dbias, "dbias", t, (c,))
         cur = self._enter()
         B.painn_layer_norm_backward(self.ctx, prec, n, c, pd, ldd, px, ldx, pw, pm, pr, po, ldo, pg, pb)
-        self._leave(cur, (dy, x, weight, mean, rstd, dx, dweight, dbias))
+        if cur is not None:
+            self._leave(cur, (dy, x, weight, mean, rstd, dx, dweight, dbias))
         return dx, dweight, dbias
 
     def _activation(self, name):
@@ -385,36 +389,39 @@ class Runtime:
         except KeyError:
             raise ValueError(f"unknown activation {name!r}: one of {', '.join(B.ACTIVATIONS)}") from None
 
-    def _offsets(self, offsets, groups):
+    def _shapes(self, x, weight, offsets):
+        """(rows, d_in, d_out, leading shape of the weights, groups, offsets' pointer)"""
         import torch
-        return self._whole(offsets, "offsets", torch.int32, (groups + 1,))
+        if x.dim() != 2 or weight.dim() != (2 if offsets is None else 3):
+            raise ValueError("x must be [rows, d_in] and weight " + ("[d_out, d_in]" if offsets is None
+                                                                     else "[groups, d_out, d_in]"))
+        n, i = x.shape
+        if offsets is None:
+            return n, i, weight.shape[0], (), 0, 0
+        g, o, _ = weight.shape
+        return n, i, o, (g,), g, self._whole(offsets, "offsets", torch.int32, (g + 1,))
 
     def _dense(self, x, weight, offsets, bias, activation, residual, keep_preact, out):
-        import torch
-        grouped = offsets is not None
-        prec = self._precision(x)
-        if x.dim() != 2 or weight.dim() != (3 if grouped else 2):
-            raise ValueError("x must be [rows, d_in] and weight " + ("[groups, d_out, d_in]" if grouped
-                                                                     else "[d_out, d_in]"))
-        n, i = x.shape
-        lead, o = tuple(weight.shape[:-2]), weight.shape[-2]
-        a = B.painn_linear_args(precision=prec, activation=self._activation(activation), rows=n, d_in=i, d_out=o)
-        a.x, a.ldx = self._rows(x, "x", x, n, i)
-        a.w = self._whole(weight, "weight", x.dtype, lead + (o, i))
-        a.bias = self._whole(bias, "bias", x.dtype, lead + (o,))
-        a.residual, a.ldr = self._rows(residual, "residual", x, n, o)
+        prec, t = self._precision(x), x.dtype
+        n, i, o, lead, groups, po = self._shapes(x, weight, offsets)
+        act = self._activation(activation)
+        px, ldx = self._rows(x, "x", t, n, i)
+        pw = self._whole(weight, "weight", t, lead + (o, i))
+        pb = self._whole(bias, "bias", t, lead + (o,))
+        pr, ldr = self._rows(residual, "residual", t, n, o)
         if out is None:
-            out = torch.empty((n, o), dtype=x.dtype, device=self.device)
-        a.y, a.ldy = self._rows(out, "out", x, n, o)
-        z = torch.empty((n, o), dtype=x.dtype, device=self.device) if keep_preact else None
-        a.z, a.ldz = self._rows(z, "z", x, n, o)
-        po = self._offsets(offsets, lead[0]) if grouped else None
+            out = x.new_empty((n, o))
+        py, ldy = self._rows(out, "out", t, n, o)
+        z = x.new_empty((n, o)) if keep_preact else None
+        pz, ldz = (z.data_ptr(), o) if keep_preact else (0, 0)
         cur = self._enter()
-        if grouped:
-            B.painn_grouped_linear(self.ctx, a, lead[0], po)
+        a = B.linear_args(prec, act, n, i, o, px, ldx, pw, pb, pr, ldr, py, ldy, pz, ldz)
+        if groups:
+            B.painn_grouped_linear(self.ctx, a, groups, po)
         else:
             B.painn_linear(self.ctx, a)
-        self._leave(cur, (x, weight, offsets, bias, residual, out, z))
+        if cur is not None:
+            self._leave(cur, (x, weight, offsets, bias, residual, out, z))
         return (out, z) if keep_preact else out
 
     def linear(self, x, weight, bias=None, activation="none", residual=None, keep_preact=False, out=None):
@@ -436,40 +443,36 @@ class Runtime:
     def _dense_backward(self, dy, x, weight, offsets, activation, preact, x_activation, x_preact, need_dx, dx,
                         dweight, dbias):
         import torch
-        grouped = offsets is not None
-        prec = self._precision(x)
-        if x.dim() != 2 or weight.dim() != (3 if grouped else 2):
-            raise ValueError("x must be [rows, d_in] and weight " + ("[groups, d_out, d_in]" if grouped
-                                                                     else "[d_out, d_in]"))
-        n, i = x.shape
-        lead, o = tuple(weight.shape[:-2]), weight.shape[-2]
-        a = B.painn_linear_backward_args(precision=prec, activation=self._activation(activation), rows=n, d_in=i,
-                                         d_out=o, x_activation=self._activation(x_activation))
-        if a.activation and preact is None:
+        prec, t = self._precision(x), x.dtype
+        n, i, o, lead, groups, po = self._shapes(x, weight, offsets)
+        act, x_act = self._activation(activation), self._activation(x_activation)
+        if act and preact is None:
             raise ValueError(f"preact is missing for activation {activation!r}")
-        if a.x_activation and need_dx and x_preact is None:
+        if x_act and need_dx and x_preact is None:
             raise ValueError(f"x_preact is missing for x_activation {x_activation!r}")
-        a.dy, a.lddy = self._rows(dy, "dy", x, n, o)
-        a.z, a.ldz = self._rows(preact, "preact", x, n, o)
-        a.x, a.ldx = self._rows(x, "x", x, n, i)
-        a.w = self._whole(weight, "weight", x.dtype, lead + (o, i))
-        a.xz, a.ldxz = self._rows(x_preact, "x_preact", x, n, i)
+        pdy, lddy = self._rows(dy, "dy", t, n, o)
+        pz, ldz = self._rows(preact, "preact", t, n, o)
+        px, ldx = self._rows(x, "x", t, n, i)
+        pw = self._whole(weight, "weight", t, lead + (o, i))
+        pxz, ldxz = self._rows(x_preact, "x_preact", t, n, i)
         if need_dx and dx is None:
-            dx = torch.empty((n, i), dtype=x.dtype, device=self.device)
+            dx = x.new_empty((n, i))
         if dweight is None:
             dweight = torch.empty_like(weight)
         if dbias is None:
-            dbias = torch.empty(lead + (o,), dtype=x.dtype, device=self.device)
-        a.dx, a.lddx = self._rows(dx, "dx", x, n, i)
-        a.dw = self._whole(dweight, "dweight", x.dtype, lead + (o, i))
-        a.dbias = self._whole(dbias, "dbias", x.dtype, lead + (o,))
-        po = self._offsets(offsets, lead[0]) if grouped else None
+            dbias = x.new_empty(lead + (o,))
+        pdx, lddx = self._rows(dx, "dx", t, n, i)
+        pdw = self._whole(dweight, "dweight", t, lead + (o, i))
+        pdb = self._whole(dbias, "dbias", t, lead + (o,))
         cur = self._enter()
-        if grouped:
-            B.painn_grouped_linear_backward(self.ctx, a, lead[0], po)
+        a = B.linear_backward_args(prec, act, n, i, o, pdy, lddy, pz, ldz, px, ldx, pw, pxz, ldxz, x_act, 0, pdx, lddx,
+                                   pdw, pdb)
+        if groups:
+            B.painn_grouped_linear_backward(self.ctx, a, groups, po)
         else:
             B.painn_linear_backward(self.ctx, a)
-        self._leave(cur, (dy, x, weight, offsets, preact, x_preact, dx, dweight, dbias))
+        if cur is not None:
+            self._leave(cur, (dy, x, weight, offsets, preact, x_preact, dx, dweight, dbias))
         return dx, dweight, dbias
 
     def linear_backward(self, dy, x, weight, activation="none", preact=None, x_activation="none", x_preact=None,
