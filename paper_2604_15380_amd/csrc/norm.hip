@@ -1,12 +1,15 @@
 // Layer norm and its reverse pass (FP32, BF16).
 //
-// A row is held in the registers of WPR waves (1 or 4), V values per lane and
-// step, NJ steps: the mean, then the variance about it, then the result, all
-// from one read of the row.  Rows too long for that are read again for each.
-// The waves walk over the rows, so that gamma and beta are loaded once per
-// wave and the reverse pass's column sums (dgamma, dbeta) stay in registers
-// until the end; each block then writes one partial row and k_norm_fold adds
-// the blocks' partials in their order.
+// A row is held in the registers of LPR lanes (16 to 64, or a block's 256), V
+// values (16 bytes) per lane and step, NJ steps: the mean, then the variance
+// about it, then the result, all from one read of the row, with the next row
+// on its way meanwhile.  Rows too long for that are read again for each.  The
+// lanes walk over the rows, so that gamma and beta are loaded once and the
+// reverse pass's column sums (dgamma, dbeta) stay in registers until the end;
+// each block then writes one partial row and k_norm_fold adds the blocks'
+// partials in their order.  Bound by memory.
+#include <type_traits>
+
 #include "ops.h"
 
 namespace {
@@ -15,66 +18,71 @@ using namespace ops;
 
 constexpr int TB = 256;
 
-// Sum over the row's WPR waves (all of a block where WPR = 4).
-template <int WPR>
+// Sum over the row's LPR lanes.
+template <int LPR>
 __device__ __forceinline__ float row_sum(float x, float* lds) {
-  x = wave_sum(x);
-  if constexpr (WPR > 1) {
+#pragma unroll
+  for (int o = (LPR < 64 ? LPR : 64) / 2; o; o >>= 1) x += __shfl_xor(x, o);
+  if constexpr (LPR > 64) {
     __syncthreads();
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
     __syncthreads();
     x = 0.f;
 #pragma unroll
-    for (int w = 0; w < WPR; ++w) x += lds[w];
+    for (int w = 0; w < LPR / 64; ++w) x += lds[w];
   }
   return x;
 }
 
-template <class T, int V, int NJ, int WPR>
-__global__ void __launch_bounds__(TB) k_norm(long long rows, int cols, const T* __restrict__ x, long long ldx,
+template <class T, int V, int NJ, int LPR>
+__global__ void __launch_bounds__(TB) k_norm(long long rows, int cols, const T* x, long long ldx,
                                              const T* __restrict__ gamma, const T* __restrict__ beta, float eps,
                                              T* y, long long ldy, float* __restrict__ mean,
                                              float* __restrict__ rstd) {
   __shared__ float lds[4];
-  constexpr int RPB = 4 / WPR;                     // rows of a block at a time
-  const int t = WPR == 1 ? threadIdx.x & 63 : threadIdx.x;
-  const int sub = WPR == 1 ? threadIdx.x >> 6 : 0;
+  constexpr int RPB = TB / LPR;                    // rows of a block at a time
+  const int t = threadIdx.x % LPR, sub = threadIdx.x / LPR;
   const float width = (float)cols;
-  float g[NJ][V], b[NJ][V];
+  float g[NJ][V], b[NJ][V], next[NJ][V];
+  const long long step = (long long)gridDim.x * RPB;
+  long long r = (long long)blockIdx.x * RPB + sub;
 #pragma unroll
   for (int j = 0; j < NJ; ++j) {
-    const int c = (j * 64 * WPR + t) * V;
+    const int c = (j * LPR + t) * V;
+    if (r < rows) load_n<V>(x + r * ldx + c, cols - c, next[j]);
     load_n<V>(gamma + c, cols - c, g[j]);
     load_n<V>(beta + c, cols - c, b[j]);
   }
-  for (long long r = (long long)blockIdx.x * RPB + sub; r < rows; r += (long long)gridDim.x * RPB) {
-    const T* xr = x + r * ldx;
+  // (y may be x: a row is read before it or any later one is written)
+  for (; r < rows; r += step) {
     float v[NJ][V];
     float s = 0.f;
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
-      const int c = (j * 64 * WPR + t) * V;
-      load_n<V>(xr + c, cols - c, v[j]);
+      const int c = (j * LPR + t) * V;
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[j][i] = next[j][i];
+      if (r + step < rows) load_n<V>(x + (r + step) * ldx + c, cols - c, next[j]);
     }
 #pragma unroll
     for (int j = 0; j < NJ; ++j)
 #pragma unroll
       for (int i = 0; i < V; ++i) s += v[j][i];
-    const float mu = row_sum<WPR>(s, lds) / width;
+    const float mu = row_sum<LPR>(s, lds) / width;
     s = 0.f;
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
-      const int c = (j * 64 * WPR + t) * V;
+      const int c = (j * LPR + t) * V;
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         v[j][i] -= mu;
         s += c + i < cols ? v[j][i] * v[j][i] : 0.f;
       }
     }
-    const float rs = 1.f / sqrtf(row_sum<WPR>(s, lds) / width + eps);
+    const float rs = 1.f / sqrtf(row_sum<LPR>(s, lds) / width + eps);
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
-      const int c = (j * 64 * WPR + t) * V;
+      const int c = (j * LPR + t) * V;
       float o[V];
 #pragma unroll
       for (int i = 0; i < V; ++i) o[i] = v[j][i] * rs * g[j][i] + b[j][i];
@@ -89,7 +97,7 @@ __global__ void __launch_bounds__(TB) k_norm(long long rows, int cols, const T* 
 
 // Rows of any length, one block each.
 template <class T>
-__global__ void __launch_bounds__(TB) k_norm_long(long long rows, int cols, const T* __restrict__ x, long long ldx,
+__global__ void __launch_bounds__(TB) k_norm_long(long long rows, int cols, const T* x, long long ldx,
                                                   const T* __restrict__ gamma, const T* __restrict__ beta, float eps,
                                                   T* y, long long ldy, float* __restrict__ mean,
                                                   float* __restrict__ rstd) {
@@ -102,13 +110,13 @@ __global__ void __launch_bounds__(TB) k_norm_long(long long rows, int cols, cons
       load<1>(xr + c, &v);
       s += v;
     }
-    const float mu = row_sum<4>(s, lds) / width;
+    const float mu = row_sum<TB>(s, lds) / width;
     s = 0.f;
     for (int c = threadIdx.x; c < cols; c += TB) {
       load<1>(xr + c, &v);
       s += (v - mu) * (v - mu);
     }
-    const float rs = 1.f / sqrtf(row_sum<4>(s, lds) / width + eps);
+    const float rs = 1.f / sqrtf(row_sum<TB>(s, lds) / width + eps);
     for (int c = threadIdx.x; c < cols; c += TB) {
       load<1>(xr + c, &v);
       load<1>(gamma + c, &g);
@@ -126,21 +134,20 @@ __global__ void __launch_bounds__(TB) k_norm_long(long long rows, int cols, cons
 // With xh = (x - mean) rstd and a = dy gamma:
 //   dx = rstd (a - mean(a) - xh mean(a xh)),  dgamma = sum dy xh,  dbeta = sum dy.
 // part: [gridDim.x][2][cols] partial column sums, or null.
-template <class T, int V, int NJ, int WPR>
+template <class T, int V, int NJ, int LPR>
 __global__ void __launch_bounds__(TB) k_norm_bwd(long long rows, int cols, const T* dy, long long lddy,
                                                  const T* __restrict__ x, long long ldx, const T* __restrict__ gamma,
                                                  const float* __restrict__ mean, const float* __restrict__ rstd,
                                                  T* dx, long long lddx, float* __restrict__ part) {
-  constexpr int RPB = 4 / WPR, W = 64 * WPR * V * NJ;
+  constexpr int RPB = TB / LPR, W = LPR * V * NJ;
   __shared__ float lds[4];
   __shared__ float acc[RPB > 1 ? W : 1];
-  const int t = WPR == 1 ? threadIdx.x & 63 : threadIdx.x;
-  const int sub = WPR == 1 ? threadIdx.x >> 6 : 0;
+  const int t = threadIdx.x % LPR, sub = threadIdx.x / LPR;
   const float width = (float)cols;
   float g[NJ][V], dg[NJ][V], db[NJ][V];
 #pragma unroll
   for (int j = 0; j < NJ; ++j) {
-    const int c = (j * 64 * WPR + t) * V;
+    const int c = (j * LPR + t) * V;
     load_n<V>(gamma + c, cols - c, g[j]);
 #pragma unroll
     for (int i = 0; i < V; ++i) dg[j][i] = db[j][i] = 0.f;
@@ -150,7 +157,7 @@ __global__ void __launch_bounds__(TB) k_norm_bwd(long long rows, int cols, const
     float d[NJ][V], h[NJ][V];
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
-      const int c = (j * 64 * WPR + t) * V;
+      const int c = (j * LPR + t) * V;
       load_n<V>(dy + r * lddy + c, cols - c, d[j]);
       load_n<V>(x + r * ldx + c, cols - c, h[j]);
     }
@@ -168,11 +175,11 @@ __global__ void __launch_bounds__(TB) k_norm_bwd(long long rows, int cols, const
         s2 += d[j][i] * h[j][i];
       }
     if (dx) {
-      s1 = row_sum<WPR>(s1, lds) / width;
-      s2 = row_sum<WPR>(s2, lds) / width;
+      s1 = row_sum<LPR>(s1, lds) / width;
+      s2 = row_sum<LPR>(s2, lds) / width;
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
-        const int c = (j * 64 * WPR + t) * V;
+        const int c = (j * LPR + t) * V;
         float o[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) o[i] = rs * (d[j][i] - s1 - h[j][i] * s2);
@@ -181,7 +188,7 @@ __global__ void __launch_bounds__(TB) k_norm_bwd(long long rows, int cols, const
     }
   }
   if (!part) return;
-  // the block's waves one after the other, then one partial row per block
+  // the block's rows one after the other, then one partial row per block
   float* p = part + (size_t)blockIdx.x * 2 * cols;
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
@@ -193,7 +200,7 @@ __global__ void __launch_bounds__(TB) k_norm_bwd(long long rows, int cols, const
           for (int j = 0; j < NJ; ++j)
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-              const int c = (j * 64 + t) * V + i;
+              const int c = (j * LPR + t) * V + i;
               const float s = k ? db[j][i] : dg[j][i];
               acc[c] = w ? acc[c] + s : s;
             }
@@ -204,7 +211,7 @@ __global__ void __launch_bounds__(TB) k_norm_bwd(long long rows, int cols, const
     } else {
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
-        const int c = (j * 64 * WPR + t) * V;
+        const int c = (j * LPR + t) * V;
         store_n<V>(p + (size_t)k * cols + c, cols - c, k ? db[j] : dg[j]);
       }
     }
@@ -228,8 +235,8 @@ __global__ void __launch_bounds__(TB) k_norm_bwd_long(long long rows, int cols, 
       s1 += d * g;
       s2 += d * g * ((h - mu) * rs);
     }
-    s1 = row_sum<4>(s1, lds) / width;
-    s2 = row_sum<4>(s2, lds) / width;
+    s1 = row_sum<TB>(s1, lds) / width;
+    s2 = row_sum<TB>(s2, lds) / width;
     for (int c = threadIdx.x; c < cols; c += TB) {
       load<1>(dy + r * lddy + c, &d);
       load<1>(x + r * ldx + c, &h);
@@ -260,22 +267,24 @@ __global__ void __launch_bounds__(TB) k_norm_cols(long long rows, int cols, cons
   part[((size_t)blockIdx.y * 2 + 1) * cols + c] = db;
 }
 
-// dgamma (blockIdx.y = 0) or dbeta (1): 64 columns per block, the partial rows
-// in 16 slices.
+// dgamma (blockIdx.y = 0) or dbeta (1): 32 columns per block, the partial rows
+// in 32 slices.
 template <class T>
 __global__ void __launch_bounds__(1024) k_norm_fold(int n, int cols, const float* __restrict__ part,
                                                     T* __restrict__ dgamma, T* __restrict__ dbeta) {
-  __shared__ float s[16][64];
-  const int q = threadIdx.x >> 6, l = threadIdx.x & 63, c = blockIdx.x * 64 + l;
+  __shared__ float s[32][33];
+  const int q = threadIdx.x >> 5, l = threadIdx.x & 31, c = blockIdx.x * 32 + l;
   float a = 0.f;
-  if (c < cols)
-    for (int k = q; k < n; k += 16) a += part[((size_t)k * 2 + blockIdx.y) * cols + c];
+  if (c < cols) {
+#pragma unroll 8
+    for (int k = q; k < n; k += 32) a += part[((size_t)k * 2 + blockIdx.y) * cols + c];
+  }
   s[q][l] = a;
   __syncthreads();
   if (q == 0 && c < cols) {
     a = 0.f;
 #pragma unroll
-    for (int k = 0; k < 16; ++k) a += s[k][l];
+    for (int k = 0; k < 32; ++k) a += s[k][l];
     store<1>((blockIdx.y ? dbeta : dgamma) + c, &a);
   }
 }
@@ -300,50 +309,62 @@ inline int grid_for(long long rows, int rpb, int most) {
   return (int)(n < most ? n : most);
 }
 
-template <class T, int V, int NJ, int WPR>
+template <class T, int V, int NJ, int LPR>
 void norm_fwd(const NormArgs& a) {
-  k_norm<T, V, NJ, WPR><<<grid_for(a.rows, 4 / WPR, NORM_GRID), TB, 0, a.ctx->stream>>>(
+  k_norm<T, V, NJ, LPR><<<grid_for(a.rows, TB / LPR, NORM_GRID), TB, 0, a.ctx->stream>>>(
       a.rows, a.cols, (const T*)a.x, a.ldx, (const T*)a.gamma, (const T*)a.beta, a.eps, (T*)a.y, a.ldy, a.mean,
       a.rstd);
 }
-template <class T, int V, int NJ, int WPR>
+template <class T, int V, int NJ, int LPR>
 void norm_bwd(const NormArgs& a, int grid, float* part) {
-  k_norm_bwd<T, V, NJ, WPR><<<grid, TB, 0, a.ctx->stream>>>(a.rows, a.cols, (const T*)a.dy, a.lddy, (const T*)a.x,
+  k_norm_bwd<T, V, NJ, LPR><<<grid, TB, 0, a.ctx->stream>>>(a.rows, a.cols, (const T*)a.dy, a.lddy, (const T*)a.x,
                                                             a.ldx, (const T*)a.gamma, a.mu, a.rs, (T*)a.dx, a.lddx,
                                                             part);
 }
 
-// Values of a row that the widest form holds: 4 waves x 64 lanes x 16 bytes,
-// 8 steps in FP32, 4 in BF16.
-constexpr int NORM_HELD = 8192;
+// The form for a row of `cols`: f(V, NJ, LPR) with the fewest lanes that hold it
+// in one step, then more steps, then a whole block.  False: too long.
+#define NORM_FORM(V, NJ, LPR) \
+  if (cols <= V * NJ * LPR) { f(std::integral_constant<int, V>(), std::integral_constant<int, NJ>(), \
+                                std::integral_constant<int, LPR>()); return true; }
+template <class T, class F>
+bool norm_form(int cols, F&& f) {
+  constexpr int V = 16 / sizeof(T);
+  NORM_FORM(V, 1, 16)
+  NORM_FORM(V, 1, 32)
+  NORM_FORM(V, 1, 64)
+  NORM_FORM(V, 2, 64)
+  NORM_FORM(V, 4, 64)
+  NORM_FORM(V, 2, 256)
+  NORM_FORM(V, 4, 256)
+  if constexpr (sizeof(T) == 4) { NORM_FORM(V, 8, 256) }
+  return false;
+}
+#undef NORM_FORM
 
 template <class T>
 painn_status run_norm(const NormArgs& a) {
-  constexpr bool B = sizeof(T) == 2;
   painn_ctx* ctx = a.ctx;
   prof_mark(ctx->prof, ctx->stream, KC_NORM, true);
-  const int c = a.cols;
-  if (c <= 256) norm_fwd<T, 4, 1, 1>(a);
-  else if (c <= 512) { if constexpr (B) norm_fwd<T, 8, 1, 1>(a); else norm_fwd<T, 4, 2, 1>(a); }
-  else if (c <= 1024) { if constexpr (B) norm_fwd<T, 8, 2, 1>(a); else norm_fwd<T, 4, 4, 1>(a); }
-  else if (c <= 2048) { if constexpr (B) norm_fwd<T, 8, 1, 4>(a); else norm_fwd<T, 4, 2, 4>(a); }
-  else if (c <= 4096) { if constexpr (B) norm_fwd<T, 8, 2, 4>(a); else norm_fwd<T, 4, 4, 4>(a); }
-  else if (c <= NORM_HELD) { if constexpr (B) norm_fwd<T, 8, 4, 4>(a); else norm_fwd<T, 4, 8, 4>(a); }
-  else
+  const bool held = norm_form<T>(a.cols, [&](auto v, auto nj, auto lpr) {
+    norm_fwd<T, decltype(v)::value, decltype(nj)::value, decltype(lpr)::value>(a);
+  });
+  if (!held)
     k_norm_long<T><<<grid_for(a.rows, 1, NORM_GRID), TB, 0, ctx->stream>>>(
-        a.rows, c, (const T*)a.x, a.ldx, (const T*)a.gamma, (const T*)a.beta, a.eps, (T*)a.y, a.ldy, a.mean, a.rstd);
+        a.rows, a.cols, (const T*)a.x, a.ldx, (const T*)a.gamma, (const T*)a.beta, a.eps, (T*)a.y, a.ldy, a.mean,
+        a.rstd);
   prof_mark(ctx->prof, ctx->stream, KC_NORM, false);
   return launched(ctx, "layer norm launch");
 }
 
 template <class T>
 painn_status run_norm_bwd(const NormArgs& a) {
-  constexpr bool B = sizeof(T) == 2;
   painn_ctx* ctx = a.ctx;
-  const int c = a.cols, rpb = c <= 1024 ? 4 : 1;
-  const bool held = c <= NORM_HELD;
-  const int grid = grid_for(a.rows, rpb, NORM_GRID_BWD);
-  const int slices = held ? grid : grid_for(a.rows, 1, 64);
+  const int c = a.cols;
+  int rpb = 0;                 // rows of a block at a time; 0: too long to hold
+  norm_form<T>(c, [&](auto, auto, auto lpr) { rpb = TB / decltype(lpr)::value; });
+  const int grid = grid_for(a.rows, rpb ? rpb : 1, NORM_GRID_BWD);
+  const int slices = rpb ? grid : grid_for(a.rows, 1, 64);
   float* part = nullptr;
   if (a.dgamma && slices) {
     const painn_status st = ops_workspace(ctx, (size_t)slices * 2 * c * sizeof(float));
@@ -351,25 +372,21 @@ painn_status run_norm_bwd(const NormArgs& a) {
     part = (float*)ctx->bws.p;
   }
   prof_mark(ctx->prof, ctx->stream, KC_NORM_BWD, true);
-  if (a.rows > 0) {
-    if (c <= 256) norm_bwd<T, 4, 1, 1>(a, grid, part);
-    else if (c <= 512) { if constexpr (B) norm_bwd<T, 8, 1, 1>(a, grid, part); else norm_bwd<T, 4, 2, 1>(a, grid, part); }
-    else if (c <= 1024) { if constexpr (B) norm_bwd<T, 8, 2, 1>(a, grid, part); else norm_bwd<T, 4, 4, 1>(a, grid, part); }
-    else if (c <= 2048) { if constexpr (B) norm_bwd<T, 8, 1, 4>(a, grid, part); else norm_bwd<T, 4, 2, 4>(a, grid, part); }
-    else if (c <= 4096) { if constexpr (B) norm_bwd<T, 8, 2, 4>(a, grid, part); else norm_bwd<T, 4, 4, 4>(a, grid, part); }
-    else if (held) { if constexpr (B) norm_bwd<T, 8, 4, 4>(a, grid, part); else norm_bwd<T, 4, 8, 4>(a, grid, part); }
-    else {
-      // the column sums first: dx may overwrite dy
-      if (part)
-        k_norm_cols<T><<<dim3((c + TB - 1) / TB, slices), TB, 0, ctx->stream>>>(
-            a.rows, c, (const T*)a.dy, a.lddy, (const T*)a.x, a.ldx, a.mu, a.rs, part);
-      if (a.dx)
-        k_norm_bwd_long<T><<<grid, TB, 0, ctx->stream>>>(a.rows, c, (const T*)a.dy, a.lddy, (const T*)a.x, a.ldx,
-                                                         (const T*)a.gamma, a.mu, a.rs, (T*)a.dx, a.lddx);
-    }
+  if (a.rows > 0 && rpb) {
+    norm_form<T>(c, [&](auto v, auto nj, auto lpr) {
+      norm_bwd<T, decltype(v)::value, decltype(nj)::value, decltype(lpr)::value>(a, grid, part);
+    });
+  } else if (a.rows > 0) {
+    // the column sums first: dx may overwrite dy
+    if (part)
+      k_norm_cols<T><<<dim3((c + TB - 1) / TB, slices), TB, 0, ctx->stream>>>(
+          a.rows, c, (const T*)a.dy, a.lddy, (const T*)a.x, a.ldx, a.mu, a.rs, part);
+    if (a.dx)
+      k_norm_bwd_long<T><<<grid, TB, 0, ctx->stream>>>(a.rows, c, (const T*)a.dy, a.lddy, (const T*)a.x, a.ldx,
+                                                       (const T*)a.gamma, a.mu, a.rs, (T*)a.dx, a.lddx);
   }
   if (a.dgamma)
-    k_norm_fold<T><<<dim3((c + 63) / 64, 2), 1024, 0, ctx->stream>>>(slices, c, part, (T*)a.dgamma, (T*)a.dbeta);
+    k_norm_fold<T><<<dim3((c + 31) / 32, 2), 1024, 0, ctx->stream>>>(slices, c, part, (T*)a.dgamma, (T*)a.dbeta);
   prof_mark(ctx->prof, ctx->stream, KC_NORM_BWD, false);
   return launched(ctx, "layer norm reverse launch");
 }

@@ -1,4 +1,4 @@
-"""Plain 64-bit forms of the head-tuning operators (CPU, torch.float64), and
+"""Plain 64-bit forms of the head-tuning operators (torch.float64), and
 the error that FP32 arithmetic may leave, for the tests."""
 import math
 
@@ -70,7 +70,8 @@ def sum_bound(k):
 def linear(x, w, bias, kind, residual, ranges):
     """y, z and the magnitude sum |x| |w| + |b| of z; w [G, o, i], bias [G, o]."""
     n, o = x.shape[0], w.shape[1]
-    z, mag = torch.zeros(n, o, dtype=torch.float64), torch.zeros(n, o, dtype=torch.float64)
+    z = torch.zeros(n, o, dtype=torch.float64, device=x.device)
+    mag = torch.zeros_like(z)
     for g, (a, b) in enumerate(ranges):
         z[a:b] = x[a:b] @ w[g].t()
         mag[a:b] = x[a:b].abs() @ w[g].t().abs()
@@ -89,7 +90,7 @@ def linear_backward(dy, z, kind, x, w, xz, x_kind, ranges):
     evaluation is relative to."""
     dz = dy * slope(z, kind) if kind != "none" else dy.clone()
     top = dy.abs() * (1.13 if kind != "none" else 1.0)
-    out = {k: torch.zeros(s, dtype=torch.float64) for k, s in
+    out = {k: torch.zeros(s, dtype=torch.float64, device=x.device) for k, s in
            (("dx", x.shape), ("dw", w.shape), ("db", w.shape[:2]), ("mdx", x.shape), ("mdw", w.shape),
             ("mdb", w.shape[:2]), ("edx", x.shape), ("edw", w.shape), ("edb", w.shape[:2]))}
     for g, (a, b) in enumerate(ranges):
