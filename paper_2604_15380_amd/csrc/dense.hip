@@ -798,21 +798,112 @@ __global__ void __launch_bounds__(256) k_few(Args g) {
   });
 }
 
-// dz = dy activation'(z), [rows][d_out] without gaps.
-template <class T>
-__global__ void __launch_bounds__(256) k_dz(long long rows, int d_out, const T* __restrict__ dy, long long lddy,
-                                            const T* __restrict__ z, long long ldz, int kind, T* __restrict__ dz) {
+// dz = dy activation'(z), rows of whole 128-byte lines, and dbias from the values
+// before they are rounded.  A block has cl x 256 / cl threads, V columns each;
+// chunks of rows and parts of dbias as for dw.
+struct DzArgs {
+  Groups gr;
+  int d_out, cl;
+  int chunk, tiles;
+  const void* dy;  long long lddy;
+  const void* z;   long long ldz;
+  void* dz;        long long lddz;
+  void* db;                          // may be null
+  float* part_b;                     // [chunk + group][d_out]
+};
+
+constexpr int DZ_TB = 256;
+template <class T, int KIND>
+__global__ void __launch_bounds__(DZ_TB) k_dz(DzArgs g) {
   constexpr int V = 16 / sizeof(T);
-  const int per = (d_out + V - 1) / V;
-  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-  if (i >= rows * per) return;
-  const long long r = i / per;
-  const int c = (int)(i - r * per) * V;
-  float d[V], s[V];
-  load_n<V>(dy + r * lddy + c, d_out - c, d);
-  load_n<V>(z + r * ldz + c, d_out - c, s);
-  mul_slope<V>(d, s, kind);
-  store_n<V>(dz + r * d_out + c, d_out - c, d);
+  __shared__ float red[DZ_TB * V];
+  const int rl = threadIdx.x / g.cl, lc = threadIdx.x - rl * g.cl, rows_at_once = DZ_TB / g.cl;
+  const int c = (blockIdx.x * g.cl + lc) * V, left = g.d_out - c;
+  const bool mine = rl < rows_at_once && c < g.lddz;
+  const int lane = threadIdx.x & 63, t = blockIdx.y, groups = g.gr.n ? g.gr.n : 1;
+  const T* __restrict__ dy = (const T*)g.dy + c;
+  const T* __restrict__ z = (const T*)g.z + c;
+  T* __restrict__ dz = (T*)g.dz + c;
+  for (int g0 = 0; g0 < groups; g0 += 64) {
+    long long lo = 0, hi = g.gr.rows;
+    int first = 0, last = -1;
+    if (g0 + lane < groups) {
+      if (g.gr.n) group_rows(g.gr, g0 + lane, lo, hi);
+      chunks_of(g.gr, g.chunk, g.tiles, lo, hi, first, last);
+    }
+    for (unsigned long long todo = __ballot(first <= t && t <= last); todo; todo &= todo - 1) {
+      const int l = __ffsll((long long)todo) - 1, grp = g0 + l;
+      const bool whole = __builtin_amdgcn_readlane(first, l) == __builtin_amdgcn_readlane(last, l);
+      long long r0 = (long long)t * g.chunk, r1 = r0 + g.chunk < g.gr.rows ? r0 + g.chunk : g.gr.rows;
+      if (g.gr.n) {
+        const long long glo = __builtin_amdgcn_readlane((int)lo, l), ghi = __builtin_amdgcn_readlane((int)hi, l);
+        r0 = glo > r0 ? glo : r0;
+        r1 = ghi < r1 ? ghi : r1;
+      }
+      float sum[V];
+#pragma unroll
+      for (int k = 0; k < V; ++k) sum[k] = 0.f;
+      if (mine && left >= V) {
+        for (long long r = r0 + rl; r < r1; r += rows_at_once) {
+          float d[V], s[V];
+          load<V>(dy + r * g.lddy, d);
+          load<V>(z + r * g.ldz, s);
+          mul_slope<V>(d, s, KIND);
+          store<V>(dz + r * g.lddz, d);
+#pragma unroll
+          for (int k = 0; k < V; ++k) sum[k] += d[k];
+        }
+      } else if (mine) {
+        for (long long r = r0 + rl; r < r1; r += rows_at_once) {
+          float d[V], s[V];
+          load_n<V>(dy + r * g.lddy, left, d);
+          load_n<V>(z + r * g.ldz, left, s);
+          mul_slope<V>(d, s, KIND);
+          store<V>(dz + r * g.lddz, d);              // (zeros past d_out: whole lines)
+#pragma unroll
+          for (int k = 0; k < V; ++k) sum[k] += d[k];
+        }
+      }
+      if (!g.db) continue;
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < V; ++k) red[threadIdx.x * V + k] = sum[k];
+      __syncthreads();
+      if (rl == 0 && mine && left > 0) {
+        for (int q = 1; q < rows_at_once; ++q)
+#pragma unroll
+          for (int k = 0; k < V; ++k) sum[k] += red[(q * g.cl + lc) * V + k];
+        if (whole) store_n<V>((T*)g.db + (size_t)grp * g.d_out + c, left, sum);
+        else store_n<V>(g.part_b + (size_t)(t + grp) * g.d_out + c, left, sum);
+      }
+    }
+  }
+}
+
+// dbias of the groups that lie in several of k_dz's chunks: 32 columns per
+// block, the parts in 32 slices.  blockIdx.y: the group.
+template <class T>
+__global__ void __launch_bounds__(1024) k_fold_bias(DzArgs g) {
+  __shared__ float red[32][33];
+  const int grp = blockIdx.y, q = threadIdx.x >> 5, l = threadIdx.x & 31, c = blockIdx.x * 32 + l;
+  long long lo = 0, hi = g.gr.rows;
+  if (g.gr.n) group_rows(g.gr, grp, lo, hi);
+  int first, last;
+  chunks_of(g.gr, g.chunk, g.tiles, lo, hi, first, last);
+  if (first == last) return;
+  float sum = 0.f;
+  if (c < g.d_out) {
+#pragma unroll 8
+    for (int k = first + q; k <= last; k += 32) sum += g.part_b[(size_t)(k + grp) * g.d_out + c];
+  }
+  red[q][l] = sum;
+  __syncthreads();
+  if (q == 0 && c < g.d_out) {
+    sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < 32; ++k) sum += red[k][l];
+    store<1>((T*)g.db + (size_t)grp * g.d_out + c, &sum);
+  }
 }
 
 // dw and dbias of the groups that lie in several chunks: their parts added in
@@ -890,7 +981,7 @@ bool launch(hipStream_t st, Args a, long long tiles, long long nt) {
       return true;
     }
   }
-  if constexpr (BM > 128 || BN > 128) return false;
+  if constexpr (BM > 128 || BN > 128) return false;       // (chosen for words_path only)
   else k_dense<T, BM, BN, WM, WN, MODE><<<dim3((unsigned)blocks), 64 * WM * WN, 0, st>>>(a);
   return true;
 }
@@ -902,7 +993,7 @@ inline long long rounds(const Groups& gr, int bm, int width, int bn, long long a
 }
 
 // FWD and DX: tiles of 128 x 128, two to a CU, or of 64 x 64 where those leave
-// CUs idle.  BF16 words: the tiles of least cost, where a round of 128 x 128
+// CUs idle.  FP32: 128 x 64 for up to two rounds of them.  BF16 words: the tiles of least cost, where a round of 128 x 128
 // counts 1, of 128 x 160 (for widths like 776 = 4.85 x 160) 1.25 and of 256 x
 // 256, one to a CU, 1.74: it moves half the bytes per product through the
 // caches.  us at 65,500 rows for 128 x 128 / 128 x 160 / 256 x 256 with the
@@ -928,7 +1019,11 @@ bool run_rows(hipStream_t st, const Args& a) {
   }
   if (rows * cols < FULL / 2)
     return launch<T, 64, 64, 2, 2, MODE>(st, a, tile_bound(a.gr, 64), ceil_div(width, 64));
-  if constexpr (sizeof(T) == 2) {
+  if constexpr (sizeof(T) == 4) {
+    // (13,800 rows 337 -> 776 71 / 61 us, its dx 88 / 75; 65,502 x 776 x 776 592 /
+    // 603 and 557 / 605)
+    if (rows * cols <= 2 * FULL) return launch<T, 128, 64, 2, 2, MODE>(st, a, rows, ceil_div(width, 64));
+  } else {
     if (words_path<MODE>(a)) {
       const double c128 = (double)rounds(a.gr, 128, width, 128, FULL);
       const double c160 = 1.25 * rounds(a.gr, 128, width, 160, FULL);
@@ -941,11 +1036,13 @@ bool run_rows(hipStream_t st, const Args& a) {
   return launch<T, 128, 128, 2, 2, MODE>(st, a, rows, cols);
 }
 
-// Chunks of the rows for dw, nt tiles each.  More of them fill the card
-// better, and each adds a part of dw to be written and read: a k-block takes
-// a block about `step` us (two blocks to a CU), a part 0.033 us per tile.  A
-// multiple of 8 in BF16: a chunk's tiles on one XCD read its rows from one L2
-// (776 -> 776, 65,502 rows: 264 us with 10 chunks over all XCDs, 132 with 8).
+// Chunks of the rows for dw, nt tiles each: of least time, where a k-block
+// takes a block about 1 us (FP32 1.5; two blocks to a CU) and a chunk's part of
+// dw 0.033 us per tile to be written and read.  A multiple of 8 in BF16: a
+// chunk's tiles on one XCD read its rows from one L2 (776 -> 776, 65,502 rows:
+// 264 us with 10 chunks over all XCDs, 132 with 8).  (Tiles of 256 x 256 in BF16
+// took 160 us where 128 x 128 took 159: half the operand bytes, but a third
+// more padding and twice the parts.)
 inline long long dw_chunks(long long rows, long long nt, int groups, bool half) {
   const int block_k = half ? 64 : 32;
   const double step = half ? 1.0 : 1.5;
@@ -991,55 +1088,83 @@ painn_status run_bwd(painn_ctx* ctx, const painn_linear_backward_args& p, int n_
   a.gr = Groups{n_groups, offsets, p.rows};
   a.d_in = p.d_in; a.d_out = p.d_out;
   a.a = p.dy; a.lda = p.lddy;
+  const hipStream_t st = ctx->stream;
+  const bool have_dz = p.activation != PAINN_ACT_NONE && p.rows > 0;
+
+  // dz and dbias
+  DzArgs z{};
+  constexpr int V = 16 / sizeof(T);
+  const long long z_ld = ceil_div(p.d_out, 8 * V) * 8 * V, z_cols = ceil_div(z_ld / V, DZ_TB);
+  size_t dz_bytes = 0, zb_bytes = 0;
+  if (have_dz) {
+    z.gr = a.gr;
+    z.d_out = p.d_out;
+    z.cl = (int)ceil_div(z_ld / V, z_cols);
+    z.lddz = z_ld;
+    // 16 blocks to a CU, at least 8 rows for each thread (65,502 x 776 BF16 from
+    // memory, us: 4,096 blocks 59, 2,048 65, 512 91)
+    const long long at_once = DZ_TB / z.cl, fill = ceil_div(4096, z_cols), few = ceil_div(p.rows, 8 * at_once);
+    const long long zc = ceil_div(p.rows, fill < few ? fill : few);
+    z.chunk = (int)(zc > (1 << 30) ? 1 << 30 : zc);
+    z.tiles = (int)ceil_div(p.rows, z.chunk);
+    z.dy = p.dy; z.lddy = p.lddy;
+    z.z = p.z; z.ldz = p.ldz;
+    z.db = p.dbias;
+    dz_bytes = align256((size_t)p.rows * z.lddz * sizeof(T));
+    zb_bytes = p.dbias ? align256((size_t)(z.tiles + G - 1) * p.d_out * sizeof(float)) : 0;
+    a.lda = z.lddz;
+  }
+
+  // dw: its tiles and chunks
+  Args d = a;
+  d.b = p.x; d.ldb = p.ldx;
+  d.out = p.dw;
+  d.db = have_dz ? nullptr : p.dbias;
   const size_t wsize = (size_t)p.d_out * p.d_in;
-  const bool big = p.d_in > 64 && p.d_out > 64;
-  const int bt = big ? 128 : 64;
+  const int bt = p.d_in > 64 && p.d_out > 64 ? 128 : 64;
   const long long nt = ceil_div(p.d_out, bt) * ceil_div(p.d_in, bt);
   const long long cut = ceil_div(p.rows, dw_chunks(p.rows, nt, n_groups, sizeof(T) == 2));
-  a.chunk = (int)(cut < 1 ? 1 : cut > (1 << 30) ? 1 << 30 : cut);
-  const long long chunks = p.rows > 0 ? ceil_div(p.rows, a.chunk) : 1;
-  const bool have_dz = p.activation != PAINN_ACT_NONE && p.rows > 0;
-  const size_t dz_bytes = have_dz ? align256((size_t)p.rows * p.d_out * sizeof(T)) : 0;
+  d.chunk = (int)(cut < 1 ? 1 : cut > (1 << 30) ? 1 << 30 : cut);
+  d.nt_in = (int)ceil_div(p.d_in, bt);
+  const long long chunks = p.rows > 0 ? ceil_div(p.rows, d.chunk) : 1;
+  d.tiles = (int)chunks;
   const bool parts = p.dw && chunks > 1;
   const size_t slots = (size_t)(chunks + G - 1);
   const size_t part_bytes = parts ? align256(slots * wsize * sizeof(float)) : 0;
-  const size_t need = dz_bytes + part_bytes + (parts ? slots * p.d_out * sizeof(float) : 0);
+  const size_t need = dz_bytes + zb_bytes + part_bytes + (parts ? slots * p.d_out * sizeof(float) : 0);
   if (need) {
-    const painn_status st = ops_workspace(ctx, need);
-    if (st != PAINN_OK) return st;
+    const painn_status ws = ops_workspace(ctx, need);
+    if (ws != PAINN_OK) return ws;
   }
   char* ws = (char*)ctx->bws.p;
-  const hipStream_t st = ctx->stream;
+  d.part = (float*)(ws + dz_bytes + zb_bytes);
+  d.part_b = (float*)(ws + dz_bytes + zb_bytes + part_bytes);
+
   prof_mark(ctx->prof, st, KC_LINEAR_BWD, true);
   bool ok = true;
   if (have_dz) {
-    const long long blocks = ceil_div(p.rows * ceil_div(p.d_out, 16 / sizeof(T)), 256);
-    ok = blocks <= 0x7fffffffLL;
-    if (ok)
-      k_dz<T><<<dim3((unsigned)blocks), 256, 0, st>>>(p.rows, p.d_out, (const T*)p.dy, p.lddy, (const T*)p.z, p.ldz,
-                                                     p.activation, (T*)ws);
-    a.a = ws;
-    a.lda = p.d_out;
+    z.dz = ws;
+    z.part_b = (float*)(ws + dz_bytes);
+    a.a = d.a = ws;
+    ok = z.tiles < 65536;
+    if (ok) {
+      const dim3 grid((unsigned)z_cols, z.tiles);
+      if (p.activation == PAINN_ACT_SILU) k_dz<T, PAINN_ACT_SILU><<<grid, DZ_TB, 0, st>>>(z);
+      else if (p.activation == PAINN_ACT_RELU) k_dz<T, PAINN_ACT_RELU><<<grid, DZ_TB, 0, st>>>(z);
+      else k_dz<T, PAINN_ACT_GELU><<<grid, DZ_TB, 0, st>>>(z);
+      if (p.dbias && z.tiles > 1) k_fold_bias<T><<<dim3((unsigned)ceil_div(p.d_out, 32), G), 1024, 0, st>>>(z);
+    }
   }
   if (ok && p.dw) {
-    Args d = a;
-    d.b = p.x; d.ldb = p.ldx;
-    d.out = p.dw;
-    d.db = p.dbias;
-    d.part = (float*)(ws + dz_bytes);
-    d.part_b = (float*)(ws + dz_bytes + part_bytes);
-    d.nt_in = (int)ceil_div(p.d_in, bt);
-    d.tiles = (int)chunks;
-    ok = big ? launch<T, 128, 128, 2, 2, DW>(st, d, chunks, nt) : launch<T, 64, 64, 2, 2, DW>(st, d, chunks, nt);
+    ok = bt == 128 ? launch<T, 128, 128, 2, 2, DW>(st, d, chunks, nt) : launch<T, 64, 64, 2, 2, DW>(st, d, chunks, nt);
     if (ok && parts) k_fold<T><<<dim3((unsigned)ceil_div(wsize, 1024), G), 256, 0, st>>>(d);
   }
   if (ok && p.dx && p.rows > 0) {
-    Args d = a;
-    d.b = p.w; d.ldb = p.d_in;
-    d.act = p.x_activation;
-    d.e = p.xz; d.lde = p.ldxz;
-    d.out = p.dx; d.ldo = p.lddx;
-    ok = run_rows<T, DX>(st, d);
+    a.b = p.w; a.ldb = p.d_in;
+    a.act = p.x_activation;
+    a.e = p.xz; a.lde = p.ldxz;
+    a.out = p.dx; a.ldo = p.lddx;
+    ok = run_rows<T, DX>(st, a);
   }
   prof_mark(ctx->prof, st, KC_LINEAR_BWD, false);
   if (!ok) return fail(ctx, PAINN_E_UNSUPPORTED, "more than 2^31 tiles");
