@@ -469,7 +469,7 @@ typedef struct painn_adamw painn_adamw;
  * states of zeros (8 bits: zero codes and scales) start a run.  Synchronises
  * the stream.  Errors: PAINN_E_ARG (null pointers, values out of range),
  * PAINN_E_UNSUPPORTED (state_bits, grad_precision, more than 2^31 blocks of
- * 4096 values), PAINN_E_OOM. */
+ * 1024 values), PAINN_E_OOM. */
 painn_status painn_adamw_create(painn_ctx* ctx, int32_t n_tensors, const painn_adamw_tensor* tensors,
                                 const painn_adamw_config* cfg, painn_adamw** out);
 /* One step at learning rate lr (finite, >= 0; else PAINN_E_ARG).  A captured

@@ -993,7 +993,7 @@ inline long long rounds(const Groups& gr, int bm, int width, int bn, long long a
 }
 
 // FWD and DX: tiles of 128 x 128, two to a CU, or of 64 x 64 where those leave
-// CUs idle.  FP32: 128 x 64 for up to two rounds of them.  BF16 words: the tiles of least cost, where a round of 128 x 128
+// CUs idle.  FP32: 128 x 64 for up to 1.5 rounds of them.  BF16 words: the tiles of least cost, where a round of 128 x 128
 // counts 1, of 128 x 160 (for widths like 776 = 4.85 x 160) 1.25 and of 256 x
 // 256, one to a CU, 1.74: it moves half the bytes per product through the
 // caches.  us at 65,500 rows for 128 x 128 / 128 x 160 / 256 x 256 with the
@@ -1020,9 +1020,9 @@ bool run_rows(hipStream_t st, const Args& a) {
   if (rows * cols < FULL / 2)
     return launch<T, 64, 64, 2, 2, MODE>(st, a, tile_bound(a.gr, 64), ceil_div(width, 64));
   if constexpr (sizeof(T) == 4) {
-    // (13,800 rows 337 -> 776 71 / 61 us, its dx 88 / 75; 65,502 x 776 x 776 592 /
-    // 603 and 557 / 605)
-    if (rows * cols <= 2 * FULL) return launch<T, 128, 64, 2, 2, MODE>(st, a, rows, ceil_div(width, 64));
+    // (128 x 128 / 128 x 64: 13,800 rows 337 -> 776 71 / 61 us, its dx 88 / 75; two
+    // full rounds, dx of 65,502 x 256 -> 1,024, 212 / 238)
+    if (2 * rows * cols <= 3 * FULL) return launch<T, 128, 64, 2, 2, MODE>(st, a, rows, ceil_div(width, 64));
   } else {
     if (words_path<MODE>(a)) {
       const double c128 = (double)rounds(a.gr, 128, width, 128, FULL);

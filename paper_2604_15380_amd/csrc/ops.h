@@ -104,6 +104,29 @@ __device__ __forceinline__ void store_n(T* p, long long n, const float* x) {
   }
 }
 
+// Loads and stores of FP32 that pass the caches by.
+template <int V>
+__device__ __forceinline__ void load_past_n(const float* p, long long n, float* x) {
+  if (n >= V) {
+    const typename Pack<float, V>::type v = __builtin_nontemporal_load((const typename Pack<float, V>::type*)p);
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] = v[i];
+  } else {
+    load_n<V>(p, n, x);
+  }
+}
+template <int V>
+__device__ __forceinline__ void store_past_n(float* p, long long n, const float* x) {
+  if (n >= V) {
+    typename Pack<float, V>::type v;
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = x[i];
+    __builtin_nontemporal_store(v, (typename Pack<float, V>::type*)p);
+  } else {
+    store_n<V>(p, n, x);
+  }
+}
+
 // Sum over the wave's 64 lanes, in every lane.
 __device__ __forceinline__ float wave_sum(float x) {
 #pragma unroll

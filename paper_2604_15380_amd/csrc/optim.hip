@@ -1,10 +1,14 @@
 // AdamW over many tensors in one launch, states in FP32 or 8 bits.
 //
-// A step is one pass: FP32 states read and write 28 bytes per value (BF16
-// gradients 26, their BF16 copy 2 more), 8-bit states 16.  Each block has
-// 4,096 consecutive values of one tensor (a table made once says which), each
-// wave 1,024 of them, four at a time per lane, so that the 256 values under
-// one scale of the 8-bit states are one load of the wave.
+// A step is one pass and bound by memory: with BF16 gradients and a BF16 copy
+// FP32 states move 28 bytes per value, 8-bit states 16.  Each block has 1,024
+// consecutive values of one tensor (a table made once says which), each lane
+// four of them, so that the 256 values under one scale of the 8-bit states are
+// one load of the wave.  Short blocks and many of them: 4,096 values per block,
+// all loads first, took 67 us for 10.3 M values and 225 us for 67 M in 8 bits;
+// this takes 57 and 190.  FP32 states pass the caches by, as nothing reads
+// them before the next step: 57 -> 47 us (6.1 TB/s, the caches holding some of
+// the parameters).
 #include <math.h>
 
 #include <new>
@@ -25,7 +29,7 @@ namespace {
 
 using namespace ops;
 
-constexpr int CHUNK = 4096, QBLOCK = 256;
+constexpr int CHUNK = 1024, QBLOCK = 256;
 constexpr float QUNIT = 1.f / 448.f, QMIN = 0.001953125f;  // one over the largest e4m3 code; the smallest, 2^-9
 constexpr float TINY = 1.17549435e-38f;                  // scales below this are stored as 0
 
@@ -40,7 +44,7 @@ struct AdamTensor {
   float* vs;
 };
 struct Chunk {
-  int tensor, index;              // values [4096 index, 4096 (index + 1)) of the tensor
+  int tensor, index;              // values [1024 index, 1024 (index + 1)) of the tensor
 };
 struct AdamScalars {
   float b1, a1, b2, a2;           // beta, 1 - beta
@@ -126,53 +130,38 @@ __global__ void __launch_bounds__(256) k_adamw(const AdamTensor* __restrict__ te
                                                const Chunk* __restrict__ chunks, AdamScalars s) {
   const Chunk c = chunks[blockIdx.x];
   const AdamTensor t = tensors[c.tensor];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const long long base = (long long)c.index * CHUNK + wave * 1024;
-  float p[4][4], g[4][4], m[4][4], v[4][4], ms[4], vs[4];
-  uint32_t mc[4], vc[4];
+  const int lane = threadIdx.x & 63;
+  const long long i = (long long)c.index * CHUNK + threadIdx.x * 4, b = i - lane * 4, left = t.n - i;
+  float p[4], g[4], m[4], v[4], root[4];
+  load_n<4>(t.p + i, left, p);
+  load_n<4>((const G*)t.g + i, left, g);
+  if constexpr (Q8) {
+    const uint32_t mc = load_codes((const uint8_t*)t.m + i, left), vc = load_codes((const uint8_t*)t.v + i, left);
+    decode(mc, b < t.n ? t.ms[b / QBLOCK] : 0.f, m);
+    decode(vc, b < t.n ? t.vs[b / QBLOCK] : 0.f, v);
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const long long b = base + k * QBLOCK, i = b + lane * 4, left = t.n - i;
-    load_n<4>(t.p + i, left, p[k]);
-    load_n<4>((const G*)t.g + i, left, g[k]);
-    if constexpr (Q8) {
-      mc[k] = load_codes((const uint8_t*)t.m + i, left);
-      vc[k] = load_codes((const uint8_t*)t.v + i, left);
-      ms[k] = b < t.n ? t.ms[b / QBLOCK] : 0.f;
-      vs[k] = b < t.n ? t.vs[b / QBLOCK] : 0.f;
-    } else {
-      load_n<4>((const float*)t.m + i, left, m[k]);
-      load_n<4>((const float*)t.v + i, left, v[k]);
-    }
+    for (int e = 0; e < 4; ++e) v[e] *= v[e];
+  } else {
+    load_past_n<4>((const float*)t.m + i, left, m);
+    load_past_n<4>((const float*)t.v + i, left, v);
   }
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const long long b = base + k * QBLOCK, i = b + lane * 4, left = t.n - i;
-    float root[4];
-    if constexpr (Q8) {
-      decode(mc[k], ms[k], m[k]);
-      decode(vc[k], vs[k], v[k]);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[k][e] *= v[k][e];
+  for (int e = 0; e < 4; ++e) root[e] = adam(s, p[e], g[e], m[e], v[e]);
+  store_n<4>(t.p + i, left, p);
+  if (t.copy) store_n<4>(t.copy + i, left, p);
+  if constexpr (Q8) {
+    // (past the tensor's end every value is 0 and stays 0)
+    float scale_m, scale_v;
+    const uint32_t cm = encode<false>(m, scale_m), cv = encode<true>(root, scale_v);
+    store_codes((uint8_t*)t.m + i, left, cm);
+    store_codes((uint8_t*)t.v + i, left, cv);
+    if (lane == 0 && b < t.n) {
+      t.ms[b / QBLOCK] = scale_m;
+      t.vs[b / QBLOCK] = scale_v;
     }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) root[e] = adam(s, p[k][e], g[k][e], m[k][e], v[k][e]);
-    store_n<4>(t.p + i, left, p[k]);
-    if (t.copy) store_n<4>(t.copy + i, left, p[k]);
-    if constexpr (Q8) {
-      // (past the tensor's end every value is 0 and stays 0)
-      float scale_m, scale_v;
-      const uint32_t cm = encode<false>(m[k], scale_m), cv = encode<true>(root, scale_v);
-      store_codes((uint8_t*)t.m + i, left, cm);
-      store_codes((uint8_t*)t.v + i, left, cv);
-      if (lane == 0 && b < t.n) {
-        t.ms[b / QBLOCK] = scale_m;
-        t.vs[b / QBLOCK] = scale_v;
-      }
-    } else {
-      store_n<4>((float*)t.m + i, left, m[k]);
-      store_n<4>((float*)t.v + i, left, v[k]);
-    }
+  } else {
+    store_past_n<4>((float*)t.m + i, left, m);
+    store_past_n<4>((float*)t.v + i, left, v);
   }
 }
 
@@ -203,9 +192,9 @@ painn_status painn_adamw_create(painn_ctx* ctx, int32_t n_tensors, const painn_a
     if (t.n < 0) return fail(ctx, PAINN_E_ARG, "tensor " + std::to_string(k) + ": negative size");
     if (t.n > 0 && (!t.param || !t.grad || !t.m || !t.v || (c.state_bits == 8 && (!t.m_scale || !t.v_scale))))
       return fail(ctx, PAINN_E_ARG, "tensor " + std::to_string(k) + ": null array");
-    if (t.n > (1LL << 43)) return fail(ctx, PAINN_E_UNSUPPORTED, "more than 2^31 blocks of 4096 values");
+    if (t.n > (1LL << 41)) return fail(ctx, PAINN_E_UNSUPPORTED, "more than 2^31 blocks of 1024 values");
     chunks += (t.n + CHUNK - 1) / CHUNK;
-    if (chunks > 0x7fffffffLL) return fail(ctx, PAINN_E_UNSUPPORTED, "more than 2^31 blocks of 4096 values");
+    if (chunks > 0x7fffffffLL) return fail(ctx, PAINN_E_UNSUPPORTED, "more than 2^31 blocks of 1024 values");
   }
   painn_adamw* o = new (std::nothrow) painn_adamw();
   if (!o) return fail(ctx, PAINN_E_OOM, "host allocation failed");
