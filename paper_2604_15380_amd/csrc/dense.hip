@@ -374,7 +374,7 @@ __device__ __forceinline__ void each_tile(const Args& g, Work&& work) {
 // wave's corner in the tile; lds: finish_floats per wave, free for use.
 template <int FN> constexpr int finish_floats() { return 16 * (FN * 16 + 4); }
 
-template <class T, int FM, int FN, int MODE>
+template <class T, int FM, int FN, int MODE, bool WORDS = false>
 __device__ __forceinline__ void finish(const Args& g, const Tile<T>& w, int wm, int wn, const f4_t (&acc)[FM][FN],
                                        const f4_t* accb, bool sum_b, float* lds) {
   constexpr int WT = FN * 16, PITCH = WT + 4, LPR = WT / 8, RPP = 64 / LPR;     // lanes per row, rows per pass
@@ -389,6 +389,22 @@ __device__ __forceinline__ void finish(const Args& g, const Tile<T>& w, int wm, 
   float bias[8];
   if (MODE == FWD && g.bias) load_n<8>((const T*)g.bias + (size_t)w.g * g.d_out + n, left, bias);
   constexpr int PASSES = (16 + RPP - 1) / RPP;
+  // xz in whole words: all of them asked for before the first is used, at
+  // addresses within the tile's rows and columns
+  constexpr bool EARLY = MODE == DX && WORDS && FM * PASSES <= 12;
+  u4_t early[EARLY ? FM : 1][EARLY ? PASSES : 1];
+  if constexpr (EARLY)
+    if (g.act != PAINN_ACT_NONE) {
+      const T* xz = (const T*)g.e + (n < w.n_end ? n : w.n_end - 8);
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int q = 0; q < PASSES; ++q) {
+          const long long m = w.m0 + wm + 16 * i + q * RPP + lane / LPR;
+          __builtin_memcpy(&early[i][q], xz + (m < w.m_end ? m : w.m_end - 1) * g.lde, 16);
+        }
+      __builtin_amdgcn_sched_barrier(0);
+    }
 #pragma unroll
   for (int i = 0; i < FM; ++i) {
 #pragma unroll
@@ -430,7 +446,14 @@ __device__ __forceinline__ void finish(const Args& g, const Tile<T>& w, int wm, 
           }
         } else if (g.act != PAINN_ACT_NONE) {
           float z[8];
-          load_n<8>((const T*)g.e + m * g.lde + n, left, z);
+          if constexpr (EARLY) {
+            T h[8];
+            __builtin_memcpy(h, &early[i][q], 16);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) z[e] = (float)h[e];
+          } else {
+            load_n<8>((const T*)g.e + m * g.lde + n, left, z);
+          }
           mul_slope<8>(v, z, g.act);
         }
         if (MODE != DW && g.past && left >= 8) store_past<8>(out + m * ldo, v);
@@ -705,7 +728,7 @@ __device__ __forceinline__ void product16(const Args& g, const Tile<b16>& w, uin
     multiply(1);
   }
   __syncthreads();
-  finish<b16, FM, FN, MODE>(g, w, wm, wn, acc, accb, sum_b, (float*)lds);
+  finish<b16, FM, FN, MODE, true>(g, w, wm, wn, acc, accb, sum_b, (float*)lds);
 }
 
 template <int BM, int BN, int WM, int WN, int MODE>
