@@ -411,8 +411,8 @@ typedef struct {
 
 /* args is a host pointer.  Errors: PAINN_E_ARG (null pointers, widths < 1,
  * rows < 0, a stride below the row's width, an unknown activation, dbias
- * without dw), PAINN_E_UNSUPPORTED (FP64; widths above 2^20; more than 2^31
- * tiles), PAINN_E_OOM (the reverse pass's workspace). */
+ * without dw), PAINN_E_UNSUPPORTED (FP64; widths above 2^20; more than 2^40
+ * rows or 2^31 tiles), PAINN_E_OOM (the reverse pass's workspace). */
 painn_status painn_linear(painn_ctx* ctx, const painn_linear_args* args);
 painn_status painn_linear_backward(painn_ctx* ctx, const painn_linear_backward_args* args);
 

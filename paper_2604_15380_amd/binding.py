@@ -340,13 +340,27 @@ class painn_adamw_config(ctypes.Structure):
                 ("weight_decay", ctypes.c_double), ("state_bits", _I32), ("grad_precision", _I32), ("steps", _I64)]
 
 
-def painn_adamw_create(ctx: int, tensors: list, cfg: dict) -> int:
-    """tensors: dicts of painn_adamw_tensor's fields (absent: null)."""
+def adamw_tensors(fields) -> bytes:
+    """painn_adamw_tensor structs from one list per field, in their order (null
+    pointers: 0)."""
+    n = len(fields[0])
+    return struct.pack("@" + "qPPPPPPP" * n, *[x for t in zip(*fields) for x in t])
+
+
+assert struct.calcsize("@qPPPPPPP") == ctypes.sizeof(painn_adamw_tensor)
+
+
+def painn_adamw_create(ctx: int, tensors, cfg: dict) -> int:
+    """tensors: dicts of painn_adamw_tensor's fields (absent: null), or
+    adamw_tensors(...)."""
     out = _P()
-    t = (painn_adamw_tensor * max(1, len(tensors)))(*[painn_adamw_tensor(**x) for x in tensors])
     c = painn_adamw_config(**cfg)
-    _check(load_library().painn_adamw_create(ctx, len(tensors), ctypes.addressof(t), ctypes.addressof(c),
-                                             ctypes.byref(out)), ctx)
+    if isinstance(tensors, bytes):
+        n, at = len(tensors) // ctypes.sizeof(painn_adamw_tensor), tensors
+    else:
+        t = (painn_adamw_tensor * max(1, len(tensors)))(*[painn_adamw_tensor(**x) for x in tensors])
+        n, at = len(tensors), ctypes.addressof(t)
+    _check(load_library().painn_adamw_create(ctx, n, at, ctypes.addressof(c), ctypes.byref(out)), ctx)
     return out.value
 
 

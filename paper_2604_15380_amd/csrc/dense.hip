@@ -4,21 +4,32 @@
 //
 // All three products are one tile kernel, D[m][n] = sum_k A[m][k] B[n][k]:
 //   forward  A = x, B = w;   dx  A = dz, B = w^T;   dw  A = dz^T, B = x^T.
-// A block stages BK values of k of both operands in LDS as [row][k] in BF16 (a
-// transposed operand is turned on the way), its waves feed 16x16x32 matrix
-// instructions from there, and the next k-block's loads are in flight
-// meanwhile.  The weights are the instruction's first operand, so that a lane
-// ends up with four neighbouring columns of one row.
+// A block stages k-blocks of both operands in LDS, its waves feed 16x16x32
+// matrix instructions from there.  The weights are the instruction's first
+// operand, so that a lane ends up with four neighbouring columns of one row;
+// the results pass through LDS once more, so that bias, activation, residual
+// and all stores work on whole pieces of rows.  BF16 operands whose rows start
+// at 16-byte words go from memory straight to LDS (k_dense16); all others and
+// FP32 pass through registers (k_dense); a few rows take k_few.
 //
 // FP32 operands become three BF16 planes on the way into LDS (split3, mfma.h)
 // and six of the nine plane products are formed: 96 matrix-core cycles per
-// 16x16x32 against 256 of the FP32 instruction, at FP32's accuracy.
+// 16x16x32 against 256 of the FP32 instruction, at FP32's accuracy (65,502 x
+// 776 x 776: 0.59 ms, a library's FP32 product 0.79 ms).
+//
+// What bounds it: with BF16 the bytes.  65,536 x 1,024 -> 1,024 takes 131 us, 1.05
+// PFLOP/s (a library's product without epilogue 103); the loads alone take
+// 121, the products alone 103.  At 776 columns a row's 128-byte piece lies in
+// two cache lines, which is most of 65,502 x 776 x 776's 110 us (with rows of
+// 832 columns 100).  FP32: the vector instructions that split the planes, 6.6
+// per value, beside 96 matrix instructions per wave and k-block.
 //
 // Rows of a ragged batch are tiled per group: a block finds its tile by a scan
 // over the groups' row counts, one group per lane, so that no launch or
-// readback plans the tiles.  dw contracts over the rows: each group's rows are
-// cut into chunks of a fixed length, one block per chunk and tile of dw, and
-// where a group has several chunks k_fold adds their FP32 parts in order.
+// readback plans the tiles.  dw contracts over the rows: the batch is cut into
+// chunks of equal length wherever the groups end, a block goes through its
+// chunk's groups one after the other, and where a group lies in several chunks
+// k_fold adds their FP32 parts in order.
 #include "mfma.h"
 #include "ops.h"
 
@@ -576,7 +587,7 @@ typedef short s4_t __attribute__((ext_vector_type(4)));
 // (the same for the wave).  Written as an instruction because the compiler
 // would wait for it before any LDS read, the other buffer's too: it knows
 // nothing of it, and wait_loads() does the waiting.  (It has no register
-// output that could be taken too early.)
+// output that could be taken too early; m0 has no other use in this file.)
 __device__ __forceinline__ void load_to_lds(const void* p, uint32_t at) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(p), "s"(at) : "memory");
 }
@@ -586,17 +597,16 @@ __device__ __forceinline__ uint32_t lds_byte(const void* p) {
 // All of this wave's loads are done, those to LDS among them.
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" : : : "memory"); }
 
-template <int R, int BK, int TH, bool TR>
+template <int R, int TH, bool TR>
 struct Dma {
-  static constexpr int CH = BK / 8, C = R / 8, UNITS = R * BK / 8, U = (UNITS + TH - 1) / TH;
+  static constexpr int BK = 64, CH = BK / 8, C = R / 8, UNITS = R * CH, U = (UNITS + TH - 1) / TH;
   static constexpr int READS = TR ? 2 : 1;      // LDS reads of a fragment
   static_assert(UNITS % 64 == 0, "whole waves of words");
   const b16* base;             // of the next k-block, the same for all lanes
   uint32_t off[U];             // this lane's words in it
 
-  // plain: how row `row`'s chunks are permuted, so that 8 rows' words of one
+  // plain: chunk c of a row lies at c ^ (row % 8), so that 8 rows' words of one
   // chunk lie in different banks
-  __device__ __forceinline__ static int turn(int row) { return CH == 8 ? row & 7 : (row >> 1) & 3; }
   // transposed: chunk c of k's row lies at (c + 2 (k % 4)) % C; the reverse
   __device__ __forceinline__ static int row_chunk(int at, int k) {
     const int c = at - 2 * (k & 3);
@@ -606,7 +616,7 @@ struct Dma {
   __device__ __forceinline__ static int first_k(int i) {
     const int u = i * TH + threadIdx.x;
     if constexpr (TR) return u / C;
-    return ((u % CH) ^ turn(u / CH)) * 8;
+    return ((u % CH) ^ ((u / CH) & 7)) * 8;
   }
   // Rows [r0, r0 + R) of n_rows (at least 1; transposed: a multiple of 8) of a
   // matrix whose row stride is below 2^22.  Rows past n_rows hold others' values.
@@ -638,7 +648,7 @@ struct Dma {
   __device__ __forceinline__ static bf8_t frag(const uint16_t* lds, int r, int kk) {
     const int lane = threadIdx.x & 63, lr = lane & 15, lq = lane >> 4;
     if constexpr (!TR) {
-      return *(const bf8_t*)(lds + (r + lr) * BK + (((4 * kk + lq) ^ turn(lr)) << 3));
+      return *(const bf8_t*)(lds + (r + lr) * BK + (((4 * kk + lq) ^ (lr & 7)) << 3));
     } else {
       const int k = 32 * kk + 8 * lq + (lr >> 2);
       int c = (r >> 3) + ((lr & 3) >> 1) + 2 * (k & 3);
@@ -657,8 +667,8 @@ template <int BM, int BN, int WM, int WN, int MODE>
 __device__ __forceinline__ void product16(const Args& g, const Tile<b16>& w, uint16_t* lds) {
   constexpr int TH = 64 * WM * WN, BK = 64, SA = BM * BK, S = SA + BN * BK;
   constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
-  using A = Dma<BM, BK, TH, MODE == DW>;
-  using B = Dma<BN, BK, TH, MODE != FWD>;
+  using A = Dma<BM, TH, MODE == DW>;
+  using B = Dma<BN, TH, MODE != FWD>;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
   const bool sum_b = MODE == DW && g.db != nullptr && w.n0 == 0 && wn == 0;
@@ -745,15 +755,25 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_dense16(Args g) {
 // ---- few rows ---------------------------------------------------------------------
 // The forward of a few rows reads its weights once and little else: a block has
 // 16 rows x 16 columns, its four waves share out k and load their fragments
-// from memory straight into registers, all of a wave's loads of 128 k at once;
+// from memory straight into registers, 8 k-blocks' loads at once (FP32: 4);
 // their sums meet in LDS.
 template <class T>
 struct Words8 {                     // 8 k of one row: 16 or 32 bytes
-  float x[8];
+  T x[8];
+  __device__ __forceinline__ void load(const T* p, long long n) {
+    if (n >= 8) {
+      __builtin_memcpy(x, p, sizeof(x));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        x[i] = (T)0.f;
+        if (i < n) x[i] = p[i];
+      }
+    }
+  }
   __device__ __forceinline__ void planes(bf8_t* f) const {
     if constexpr (sizeof(T) == 2) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) f[0][i] = (b16)x[i];      // (exact)
+      __builtin_memcpy(f, x, 16);
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -769,7 +789,7 @@ struct Words8 {                     // 8 k of one row: 16 or 32 bytes
 template <class T>
 __global__ void __launch_bounds__(256) k_few(Args g) {
   using M = Mma<T>;
-  constexpr int NP = M::NP, AHEAD = 4;
+  constexpr int NP = M::NP, AHEAD = sizeof(T) == 2 ? 8 : 4;
   __shared__ f4_t sums[4][64];
   each_tile<T, 16, 16, FWD>(g, [&](const Tile<T>& w) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -783,8 +803,8 @@ __global__ void __launch_bounds__(256) k_few(Args g) {
 #pragma unroll
       for (int i = 0; i < AHEAD; ++i) {
         const long long k = k0 + 128 * i + 8 * lq;
-        load_n<8>(pa + k, w.nk - k, a[i].x);
-        load_n<8>(pb + k, w.nk - k, b[i].x);
+        a[i].load(pa + k, w.nk - k);
+        b[i].load(pb + k, w.nk - k);
       }
 #pragma unroll
       for (int i = 0; i < AHEAD; ++i) {
@@ -1203,7 +1223,8 @@ painn_status dense_check(painn_ctx* ctx, int prec, int act, int x_act, int64_t r
   if (!known_act(act) || !known_act(x_act)) return fail(ctx, PAINN_E_ARG, "unknown activation");
   if (d_in < 1 || d_out < 1) return fail(ctx, PAINN_E_ARG, "widths must be at least 1");
   if (rows < 0) return fail(ctx, PAINN_E_ARG, "rows must not be negative");
-  if (d_in > (1 << 20) || d_out > (1 << 20)) return fail(ctx, PAINN_E_UNSUPPORTED, "widths above 2^20");
+  if (d_in > (1 << 20) || d_out > (1 << 20) || rows > (1LL << 40))
+    return fail(ctx, PAINN_E_UNSUPPORTED, "widths above 2^20 or more than 2^40 rows");
   if (grouped) {
     if (n_groups < 1 || n_groups > 4096) return fail(ctx, PAINN_E_ARG, "n_groups must be in [1, 4096]");
     if (!offsets) return fail(ctx, PAINN_E_ARG, "null offsets");

@@ -95,38 +95,45 @@ class AdamW:
         held = torch.float8_e4m3fn if small else torch.float32
         blocks = [-(-p.numel() // 256) for p in params]
         if state is None:
-            new = lambda sizes, t: [torch.zeros(n, dtype=torch.uint8 if t == held and small else t,  # noqa: E731
-                                                device=rt.device).view(t) for n in sizes]
-            sizes = [p.numel() for p in params]
-            state = dict(m=new(sizes, held), v=new(sizes, held))
+            def zeros(sizes, dtype):
+                return [torch.zeros(n * (1 if dtype is held and small else 4), dtype=torch.uint8,
+                                    device=rt.device).view(dtype) for n in sizes]
+            values = [p.numel() for p in params]
+            state = dict(m=zeros(values, held), v=zeros(values, held))
             if small:
-                state.update(m_scale=new(blocks, torch.float32), v_scale=new(blocks, torch.float32))
+                state.update(m_scale=zeros(blocks, torch.float32), v_scale=zeros(blocks, torch.float32))
         self.rt, self.params, self.grads, self.copies = rt, params, grads, copies
         self.state_bits, self.lr = state_bits, lr
         self.m, self.v = list(state["m"]), list(state["v"])
         self.m_scale = list(state["m_scale"]) if small else None
         self.v_scale = list(state["v_scale"]) if small else None
-        tensors = []
-        for k, (p, g, c) in enumerate(zip(params, grads, copies)):
-            n = p.numel()
-            t = dict(n=n)
-            fields = [("param", p, torch.float32, n), ("grad", g, gt, n), ("copy", c, torch.bfloat16, n),
-                      ("m", self.m[k], held, n), ("v", self.v[k], held, n)]
-            if small:
-                fields += [("m_scale", self.m_scale[k], torch.float32, blocks[k]),
-                           ("v_scale", self.v_scale[k], torch.float32, blocks[k])]
-            for name, a, dtype, size in fields:
-                if a is None:
+        # a field per list, as painn_adamw_tensor orders them
+        lists = [("param", params, torch.float32, 1), ("grad", grads, gt, 1), ("copy", copies, torch.bfloat16, 1),
+                 ("m", self.m, held, 1), ("v", self.v, held, 1)]
+        if small:
+            lists += [("m_scale", self.m_scale, torch.float32, 256), ("v_scale", self.v_scale, torch.float32, 256)]
+        sizes = [p.numel() for p in params]
+        fields, dev = [sizes], rt.device
+        for name, arrays, dtype, per in lists:
+            if len(arrays) != len(sizes):
+                raise ValueError(f"{len(arrays)} arrays of {name} for {len(sizes)} tensors")
+            ptrs = []
+            for k, (a, n) in enumerate(zip(arrays, sizes)):
+                if a is None and name == "copy":
+                    ptrs.append(0)
                     continue
-                if a.dtype != dtype or a.numel() != size or not a.is_contiguous() or a.device != rt.device:
-                    raise ValueError(f"tensor {k}: {name} must be contiguous {dtype} of {size} values on {rt.device}")
-                t[name] = a.data_ptr() or None
-            tensors.append(t)
+                n = -(-n // per)
+                if a.dtype is not dtype or a.numel() != n or not a.is_contiguous() or a.device != dev:
+                    raise ValueError(f"tensor {k}: {name} must be contiguous {dtype} of {n} values on {dev}")
+                ptrs.append(a.data_ptr())
+            fields.append(ptrs)
+        while len(fields) < 8:
+            fields.append([0] * len(sizes))
         self.handle = 0
         cfg = dict(beta1=betas[0], beta2=betas[1], eps=eps, weight_decay=weight_decay, state_bits=state_bits,
                    grad_precision=B.PAINN_BF16 if gt == torch.bfloat16 else B.PAINN_FP32, steps=steps)
         cur = rt._enter()
-        self.handle = B.painn_adamw_create(rt.ctx, tensors, cfg)
+        self.handle = B.painn_adamw_create(rt.ctx, B.adamw_tensors(fields), cfg)
         rt._leave(cur, ())
 
     def step(self, lr=None):
