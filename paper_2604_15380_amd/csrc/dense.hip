@@ -1036,8 +1036,8 @@ inline long long rounds(const Groups& gr, int bm, int width, int bn, long long a
 }
 
 // FWD and DX: tiles of 128 x 128, two to a CU, or of 64 x 64 where those leave
-// CUs idle.  FP32: 128 x 64 for up to 1.5 rounds of them.  BF16 words: the tiles of least cost, where a round of 128 x 128
-// counts 1, of 128 x 160 (for widths like 776 = 4.85 x 160) 1.25 and of 256 x
+// CUs idle.  FP32: 128 x 64 for up to 1.5 rounds of them.  BF16 words: the
+// tiles of least cost, where a round of 128 x 128 counts 1, of 128 x 160 (for widths like 776 = 4.85 x 160) 1.25 and of 256 x
 // 256, one to a CU, 1.74: it moves half the bytes per product through the
 // caches.  us at 65,500 rows for 128 x 128 / 128 x 160 / 256 x 256 with the
 // costs in brackets: 776 -> 776 134 / 119 / 131 (7 / 6.3 / 7); 1,024 -> 1,024
@@ -1049,9 +1049,12 @@ bool run_rows(hipStream_t st, const Args& a) {
   const int width = MODE == FWD ? a.d_out : a.d_in;
   const long long rows = tile_bound(a.gr, 128), cols = ceil_div(width, 128);
   if constexpr (MODE == FWD) {
-    // (up to 128 rows of 776: 7.9 to 8.5 us against 10.6 in tiles of 64 x 64,
-    // FP32 13 to 18 against 36; at 512 rows 14.6 against 10.9, 39 against 37)
-    if (tile_bound(a.gr, 16) * ceil_div(width, 16) <= FULL) {
+    // Its blocks' waves split the inner dimension, which has to be long enough
+    // to be worth it (us, k_few / tiles of 64 x 64, 32 rows to 776 columns: BF16
+    // inner 64 8.9 / 6.3, 256 7.8 / 7.1, 384 7.3 / 7.8, 776 6.6 / 10.6; FP32 128
+    // 9.8 / 9.1, 192 9.5 / 10.7, 776 14 / 27; 512 rows of 776 11.8 / 11.0, FP32
+    // 38 / 27; each with 2 us of the events around it)
+    if (a.d_in > (sizeof(T) == 2 ? 256 : 128) && tile_bound(a.gr, 16) * ceil_div(width, 16) <= FULL) {
       Args b = a;
       b.tiles = (int)tile_bound(a.gr, 16);
       b.nt = (int)ceil_div(width, 16);

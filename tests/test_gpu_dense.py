@@ -297,3 +297,10 @@ def test_refusals(rt):
         with pytest.raises(B.PainnError) as e:
             B.painn_linear_backward(rt.ctx, B.painn_linear_backward_args(**{**back, **kw}))
         assert e.value.status == -1, kw
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("i", [127, 128, 129, 136, 255, 256, 257, 264, 1030])
+def test_few_rows_of_any_inner_length(rt, dtype, i):
+    forward_case(rt, dtype, 19, i, 45, "silu", True, True, seed=i)
+    forward_case(rt, dtype, 33, i, 40, "gelu", True, True, [0, 0, 1, 18, 18, 33], seed=i + 1)
