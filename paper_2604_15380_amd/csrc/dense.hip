@@ -305,6 +305,7 @@ struct Args {
   int tiles;                         // FWD, DX: row tiles (an upper bound); DW: chunks (at least 1)
   int nt;                            // column tiles of a row tile; DW: tiles of dw
   int nt_in;                         // DW: tiles along d_in
+  long long rest;                    // DX, DW in tiles of 64 x 64: from dz to its remainders, 0: none
   bool past, past_z;                 // whether out and z are stored past the caches
 };
 
@@ -510,17 +511,24 @@ __device__ __forceinline__ void product(const Args& g, const Tile<T>& w, uint16_
   Stage<T, BM, TH, MODE == DW> sa;
   Stage<T, BN, TH, MODE != FWD> sb;
   const long long nk = w.nk;
+  const T* a = w.a;
   if (nk > 0) {
-    sa.load(w.a, g.lda, w.m0, w.m_end, 0, nk);
+    sa.load(a, g.lda, w.m0, w.m_end, 0, nk);
     sb.load(w.b, g.ldb, w.n0, w.n_end, 0, nk);
   }
-  for (long long k0 = 0; k0 < nk; k0 += BK) {
+  for (long long k0 = 0; k0 < nk;) {
+    k0 += BK;
+    if constexpr (MODE != FWD && BM == 64 && sizeof(T) == 2)
+      if (k0 >= nk && g.rest && a == w.a) {      // once more, with the remainders
+        a += g.rest;
+        k0 = 0;
+      }
     sa.put(As);
     sb.put(Bs);
     __syncthreads();
-    if (k0 + BK < nk) {
-      sa.load(w.a, g.lda, w.m0, w.m_end, k0 + BK, nk);
-      sb.load(w.b, g.ldb, w.n0, w.n_end, k0 + BK, nk);
+    if (k0 < nk) {
+      sa.load(a, g.lda, w.m0, w.m_end, k0, nk);
+      sb.load(w.b, g.ldb, w.n0, w.n_end, k0, nk);
     }
 #pragma unroll
     for (int kk = 0; kk < BK / 32; ++kk) {
@@ -694,11 +702,20 @@ __device__ __forceinline__ void product16(const Args& g, const Tile<b16>& w, uin
     sb.next(lds + buf * S + SA, g.ldb, from);
   };
   if (left > 0) fetch(0, left);
-  for (int cur = 0; left > 0; cur ^= 1, left -= BK) {
+  bool again = MODE != FWD && g.rest != 0;
+  for (int cur = 0; left > 0; cur ^= 1) {
     // everybody's words of this block are there, and nobody reads the other buffer
     wait_loads();
     __syncthreads();
-    if (left > BK) fetch(cur ^ 1, left - BK);
+    left -= BK;
+    if constexpr (MODE != FWD && BM == 64)
+      if (left <= 0 && again) {                  // once more, with the remainders
+        again = false;
+        left = w.nk;
+        sa.init(w.a + g.rest, g.lda, w.m0, w.m_end);
+        sb.init(w.b, g.ldb, w.n0, w.n_end);
+      }
+    if (left > 0) fetch(cur ^ 1, left);
     const uint16_t *a = lds + cur * S, *b = a + SA;
     bf8_t fa[2][FM], fb[2][FN];
     auto read = [&](int kk) {
@@ -841,8 +858,9 @@ __global__ void __launch_bounds__(256) k_few(Args g) {
   });
 }
 
-// dz = dy activation'(z), rows of whole 128-byte lines, and dbias from the values
-// before they are rounded.  A block has cl x 256 / cl threads, V columns each;
+// dz = dy activation'(z), rows of whole 128-byte lines, what its rounding to BF16
+// leaves of it where g.rest asks, and dbias from the values before they are
+// rounded.  A block has cl x 256 / cl threads, V columns each;
 // chunks of rows and parts of dbias as for dw.
 struct DzArgs {
   Groups gr;
@@ -851,9 +869,24 @@ struct DzArgs {
   const void* dy;  long long lddy;
   const void* z;   long long ldz;
   void* dz;        long long lddz;
+  long long rest;                    // from dz to its remainders, 0: none
   void* db;                          // may be null
   float* part_b;                     // [chunk + group][d_out]
 };
+
+// What is left of values rounded to T; 0 where that is not finite.
+template <class T, int V>
+__device__ __forceinline__ void store_rest(T* p, const float* d) {
+  if constexpr (sizeof(T) == 2) {
+    float r[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      const float h = (float)(T)d[k];
+      r[k] = __builtin_isfinite(h) ? d[k] - h : 0.f;
+    }
+    store<V>(p, r);
+  }
+}
 
 constexpr int DZ_TB = 256;
 template <class T, int KIND>
@@ -893,6 +926,7 @@ __global__ void __launch_bounds__(DZ_TB) k_dz(DzArgs g) {
           load<V>(z + r * g.ldz, s);
           mul_slope<V>(d, s, KIND);
           store<V>(dz + r * g.lddz, d);
+          if (g.rest) store_rest<T, V>(dz + r * g.lddz + g.rest, d);
 #pragma unroll
           for (int k = 0; k < V; ++k) sum[k] += d[k];
         }
@@ -903,6 +937,7 @@ __global__ void __launch_bounds__(DZ_TB) k_dz(DzArgs g) {
           load_n<V>(z + r * g.ldz, left, s);
           mul_slope<V>(d, s, KIND);
           store<V>(dz + r * g.lddz, d);              // (zeros past d_out: whole lines)
+          if (g.rest) store_rest<T, V>(dz + r * g.lddz + g.rest, d);
 #pragma unroll
           for (int k = 0; k < V; ++k) sum[k] += d[k];
         }
@@ -1063,7 +1098,7 @@ bool run_rows(hipStream_t st, const Args& a) {
       return true;
     }
   }
-  if (rows * cols < FULL / 2)
+  if (rows * cols < FULL / 2 || (MODE == DX && a.rest))
     return launch<T, 64, 64, 2, 2, MODE>(st, a, tile_bound(a.gr, 64), ceil_div(width, 64));
   if constexpr (sizeof(T) == 4) {
     // (128 x 128 / 128 x 64: 13,800 rows 337 -> 776 71 / 61 us, its dx 88 / 75; two
@@ -1156,7 +1191,16 @@ painn_status run_bwd(painn_ctx* ctx, const painn_linear_backward_args& p, int n_
     z.dy = p.dy; z.lddy = p.lddy;
     z.z = p.z; z.ldz = p.ldz;
     z.db = p.dbias;
-    dz_bytes = align256((size_t)p.rows * z.lddz * sizeof(T));
+    // One rounding of dz to BF16 is one relative error of a whole row of dx and
+    // of dw's.  Over many values it adds as much again as the rounding of the
+    // result (1.4 times its error), but over a few, as in an energy's readout
+    // of 28 rows, 2.1 times.  So up to 8,192 values their remainders go through
+    // the products too (us, without / with: 28 x 257 -> 1 18 / 22, 8 x 776 -> 776
+    // 22 / 27, 120 x 64 -> 64 15 / 17, 8,192 x 776 -> 1 53 / 77; beyond the limit,
+    // 65,502 x 776 -> 1, 164 / 282).
+    if (sizeof(T) == 2 && (p.dx || p.dw) && p.rows <= 8192 / p.d_out) z.rest = p.rows * z.lddz;
+    dz_bytes = align256((size_t)(z.rest ? 2 : 1) * p.rows * z.lddz * sizeof(T));
+    a.rest = z.rest;
     zb_bytes = p.dbias ? align256((size_t)(z.tiles + G - 1) * p.d_out * sizeof(float)) : 0;
     a.lda = z.lddz;
   }
@@ -1167,7 +1211,7 @@ painn_status run_bwd(painn_ctx* ctx, const painn_linear_backward_args& p, int n_
   d.out = p.dw;
   d.db = have_dz ? nullptr : p.dbias;
   const size_t wsize = (size_t)p.d_out * p.d_in;
-  const int bt = p.d_in > 64 && p.d_out > 64 ? 128 : 64;
+  const int bt = p.d_in > 64 && p.d_out > 64 && !a.rest ? 128 : 64;
   const long long nt = ceil_div(p.d_out, bt) * ceil_div(p.d_in, bt);
   const long long cut = ceil_div(p.rows, dw_chunks(p.rows, nt, n_groups, sizeof(T) == 2));
   d.chunk = (int)(cut < 1 ? 1 : cut > (1 << 30) ? 1 << 30 : cut);

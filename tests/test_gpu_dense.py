@@ -304,3 +304,39 @@ def test_refusals(rt):
 def test_few_rows_of_any_inner_length(rt, dtype, i):
     forward_case(rt, dtype, 19, i, 45, "silu", True, True, seed=i)
     forward_case(rt, dtype, 33, i, 40, "gelu", True, True, [0, 0, 1, 18, 18, 33], seed=i + 1)
+
+
+@pytest.mark.parametrize("n,i,o,offsets", [(28, 257, 1, None), (5, 64, 1, None), (1, 776, 776, None),
+                                           (40, 130, 200, None), (8192, 40, 1, None), (128, 72, 64, [0, 1, 1, 90, 126]),
+                                           (129, 45, 37, [0, 2, 60, 60, 129])])
+def test_few_values_of_dz_are_not_rounded(rt, n, i, o, offsets):
+    # dz as a BF16 value and a BF16 remainder is 2^-16 off, E16 squared
+    t, mk = torch.bfloat16, maker(n + i, torch.bfloat16)
+    G = len(offsets) - 1 if offsets else 1
+    dy, z, x, w = mk(n, o), mk(n, o, scale=2.0), mk(n, i), mk(G, o, i, scale=o ** -0.5)
+    ranges = ref.spans(offsets, n) if offsets else [(0, n)]
+    r = ref.linear_backward(dy.double(), z.double(), "silu", x.double(), w.double(), None, "none", ranges)
+    how = dict(activation="silu", preact=z.cuda())
+    if offsets:
+        got = rt.grouped_linear_backward(dy.cuda(), x.cuda(), w.cuda(), torch.tensor(offsets, dtype=torch.int32).cuda(), **how)
+    else:
+        got = rt.linear_backward(dy.cuda(), x.cuda(), w[0].cuda(), **how)
+    inside = torch.zeros(n, dtype=torch.bool)
+    for a, e in ranges:
+        inside[a:e] = True
+    rows = max([e - a for a, e in ranges] + [1])
+    for name, mine, k in (("dx", got[0], o), ("dw", got[1], rows)):
+        mine = mine.cpu().double().reshape(r[name].shape)
+        tol = (sum_bound(2 * k) + E16 * E16) * r["m" + name] + 16 * E32 * r["e" + name] + E16 * r[name].abs()
+        err = mine - r[name]
+        within(err[inside] if name == "dx" else err, tol[inside] if name == "dx" else tol, name)
+
+
+def test_infinite_gradients_stay_infinite(rt):
+    dy = torch.ones(3, 8, dtype=torch.bfloat16)
+    dy[1, 2] = float("inf")
+    z, x, w = torch.full((3, 8), 2.0), torch.ones(3, 16), torch.ones(8, 16)
+    z, x, w = (a.to(torch.bfloat16).cuda() for a in (z, x, w))
+    dx, dw, db = rt.linear_backward(dy.cuda(), x, w, activation="silu", preact=z)
+    assert torch.isinf(dx[1]).all() and torch.isfinite(dx[0]).all() and torch.isfinite(dx[2]).all()
+    assert torch.isinf(dw[2]).all() and torch.isfinite(dw[:2]).all() and torch.isinf(db[2])
