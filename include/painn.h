@@ -387,7 +387,8 @@ typedef struct {
  * x_activation(xz) came from, dx is the gradient of xz: (dz w)
  * x_activation'(xz), in the same pass.  The residual's gradient is dy.  In
  * BF16 dz is rounded to BF16 before the products where there is an
- * activation.  relu'(0) = 0. */
+ * activation and rows * d_out is above 8,192; fewer values are held to 16 bits
+ * (a value and its remainder).  relu'(0) = 0. */
 typedef struct {
   int32_t precision, activation;
   int64_t rows;
