@@ -27,6 +27,30 @@ def dataset_order(dataset_id) -> np.ndarray:
     return np.argsort(np.asarray(dataset_id), kind="stable")
 
 
+SUM_WIDTH = 64
+
+
+def _sum_levels(ptr):
+    """The structures' sums as levels of fixed rows: of each level, which values
+    of the level before a row adds, at most SUM_WIDTH consecutive ones of one
+    structure; places past them hold the index behind the last value.  The last
+    level has one row per structure."""
+    begin, count, levels = ptr[:-1], np.diff(ptr), []
+    while True:
+        total = int(begin[-1] + count[-1]) if len(count) else 0
+        last = count.max(initial=0) <= SUM_WIDTH
+        rows = np.ones_like(count) if last else -(-count // SUM_WIDTH)
+        start = np.cumsum(rows) - rows
+        inner = np.arange(rows.sum()) - np.repeat(start, rows)       # the row's place in its structure
+        width = max(1, int(count.max(initial=0))) if last else SUM_WIDTH
+        first = inner * SUM_WIDTH
+        place = first[:, None] + np.arange(width)
+        levels.append(np.where(place < np.repeat(count, rows)[:, None], np.repeat(begin, rows)[:, None] + place, total))
+        if last:
+            return levels
+        begin, count = start, rows
+
+
 class HeadTuner:
     """weights: the model's arrays by name (shared{m}.w, shared{m}.b,
     head{h}.{m}.w, head{h}.{m}.b, as the weight file orders them).  F: the
@@ -80,7 +104,7 @@ class HeadTuner:
         cuts = ptr[np.searchsorted(ids, np.arange(self.n_heads + 1))]
         dev = self.rt.device
         return dict(s=features.to(self.dtype).contiguous(), offsets=torch.as_tensor(cuts, dtype=torch.int32).to(dev),
-                    ptr=torch.as_tensor(ptr).to(dev),
+                    ptr=torch.as_tensor(ptr).to(dev), sums=[torch.as_tensor(k).to(dev) for k in _sum_levels(ptr)],
                     structure=torch.as_tensor(np.repeat(np.arange(len(ids)), np.diff(ptr))).to(dev))
 
     # ---- forward ---------------------------------------------------------
@@ -110,11 +134,13 @@ class HeadTuner:
 
     @staticmethod
     def _sum(b, e):
-        """Energies of the structures: differences of a running sum in FP64,
+        """Energies of the structures in FP64, each from its own atoms alone,
         the same order in every call."""
         import torch
-        total = torch.cat([e.new_zeros(1, dtype=torch.float64), e.double().view(-1).cumsum(0)])
-        return total[b["ptr"][1:]] - total[b["ptr"][:-1]]
+        v = e.double().view(-1)
+        for rows in b["sums"]:
+            v = torch.cat([v, v.new_zeros(1)])[rows].sum(1)
+        return v
 
     def energies(self, b):
         return self._sum(b, self._forward(b, False)[0])
