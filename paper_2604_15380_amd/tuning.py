@@ -147,10 +147,14 @@ class HeadTuner:
 
     # ---- a step ----------------------------------------------------------
     def gradients(self, b, energy_ref):
-        """The loss, mean |E - energy_ref|; its gradients go to self.grad.
-        Gradients of the features are not formed."""
+        """The loss, mean |E - energy_ref| (energy_ref [structures], or one
+        number); its gradients go to self.grad.  Gradients of the features are
+        not formed."""
         import torch
         rt, w, g = self.rt, self.weight, self.grad
+        want = (len(b["ptr"]) - 1,)
+        if tuple(getattr(energy_ref, "shape", ())) not in ((), want):
+            raise ValueError(f"energy_ref must be {list(want)}, not {list(energy_ref.shape)}")
         e, kept = self._forward(b, True)
         diff = self._sum(b, e) - energy_ref
         sign = torch.sign(diff) / max(1, diff.numel())
