@@ -474,7 +474,9 @@ typedef struct painn_adamw painn_adamw;
 painn_status painn_adamw_create(painn_ctx* ctx, int32_t n_tensors, const painn_adamw_tensor* tensors,
                                 const painn_adamw_config* cfg, painn_adamw** out);
 /* One step at learning rate lr (finite, >= 0; else PAINN_E_ARG).  A captured
- * step repeats with the lr and step number of its capture. */
+ * step repeats with the lr and step number of its capture.  After
+ * painn_destroy of its context an optimizer refuses every step (PAINN_E_ARG)
+ * and can still be freed. */
 painn_status painn_adamw_step(painn_adamw* opt, double lr);
 /* Steps made so far (host). */
 painn_status painn_adamw_steps(const painn_adamw* opt, int64_t* steps);

@@ -182,6 +182,8 @@ struct painn_ctx {
   Workspace ws;
   // reverse-pass workspace (saved activations and gradients; grown on demand)
   Workspace bws;
+  // its optimizers (optim.hip): one may outlive the context
+  painn_adamw* optimizers = nullptr;
 };
 
 struct painn_model {

@@ -12,6 +12,9 @@ enum OpsKernelClass { KC_NORM = KC_COUNT, KC_NORM_BWD, KC_LINEAR, KC_LINEAR_BWD,
 // where it cannot be had, or only by allocating while the stream is captured.
 painn_status ops_workspace(painn_ctx* ctx, size_t need);
 
+// The context ends: its optimizers refuse every further step.
+void adamw_detach(painn_ctx* ctx);
+
 namespace ops {
 
 inline painn_status fail(painn_ctx* ctx, painn_status st, const std::string& msg) {

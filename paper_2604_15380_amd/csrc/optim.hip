@@ -15,7 +15,8 @@
 #include "ops.h"
 
 struct painn_adamw {
-  painn_ctx* ctx = nullptr;
+  painn_ctx* ctx = nullptr;       // null: the context has been destroyed
+  painn_adamw *prev = nullptr, *next = nullptr;      // of the context's optimizers
   painn_adamw_config cfg{};
   int64_t steps = 0;
   long long chunks = 0;
@@ -198,6 +199,9 @@ painn_status painn_adamw_create(painn_ctx* ctx, int32_t n_tensors, const painn_a
   painn_adamw* o = new (std::nothrow) painn_adamw();
   if (!o) return fail(ctx, PAINN_E_OOM, "host allocation failed");
   o->ctx = ctx;
+  o->next = ctx->optimizers;
+  if (o->next) o->next->prev = o;
+  ctx->optimizers = o;
   o->cfg = c;
   o->steps = c.steps;
   o->chunks = chunks;
@@ -205,7 +209,7 @@ painn_status painn_adamw_create(painn_ctx* ctx, int32_t n_tensors, const painn_a
     const size_t head = align256((size_t)n_tensors * sizeof(AdamTensor)), bytes = head + (size_t)chunks * sizeof(Chunk);
     unsigned char* host = new (std::nothrow) unsigned char[bytes]();
     if (!host) {
-      delete o;
+      painn_adamw_free(o);
       return fail(ctx, PAINN_E_OOM, "host allocation failed");
     }
     AdamTensor* ht = (AdamTensor*)host;
@@ -232,7 +236,7 @@ painn_status painn_adamw_create(painn_ctx* ctx, int32_t n_tensors, const painn_a
 }
 
 painn_status painn_adamw_step(painn_adamw* opt, double lr) {
-  if (!opt) return PAINN_E_ARG;
+  if (!opt || !opt->ctx) return PAINN_E_ARG;
   painn_ctx* ctx = opt->ctx;
   ctx->err.clear();
   if (!finite_at_least(lr, 0.0)) return fail(ctx, PAINN_E_ARG, "lr must be finite and not negative");
@@ -272,6 +276,9 @@ painn_status painn_adamw_free(painn_adamw* opt) {
   if (opt->ctx) {
     (void)hipSetDevice(opt->ctx->device);
     (void)hipStreamSynchronize(opt->ctx->stream);
+    if (opt->prev) opt->prev->next = opt->next;
+    else opt->ctx->optimizers = opt->next;
+    if (opt->next) opt->next->prev = opt->prev;
   }
   if (opt->table) (void)hipFree(opt->table);
   delete opt;
@@ -279,3 +286,12 @@ painn_status painn_adamw_free(painn_adamw* opt) {
 }
 
 }  // extern "C"
+
+void adamw_detach(painn_ctx* ctx) {
+  for (painn_adamw *o = ctx->optimizers, *next; o; o = next) {
+    next = o->next;
+    o->ctx = nullptr;
+    o->prev = o->next = nullptr;
+  }
+  ctx->optimizers = nullptr;
+}

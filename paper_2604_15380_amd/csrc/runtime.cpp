@@ -561,6 +561,7 @@ painn_status painn_destroy(painn_ctx* ctx) {
   if (ctx->bws.p) (void)hipFree(ctx->bws.p);
   if (ctx->h_status) (void)hipHostFree(ctx->h_status);
   prof_free(ctx->prof);
+  adamw_detach(ctx);
   delete ctx;
   return PAINN_OK;
 }

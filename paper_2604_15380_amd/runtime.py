@@ -157,7 +157,7 @@ class AdamW:
         return d
 
     def free(self):
-        if self.handle and self.rt.ctx:
+        if self.handle:
             B.painn_adamw_free(self.handle)
         self.handle = 0
 
