@@ -330,7 +330,9 @@ painn_status painn_trainer_free(painn_trainer* tr);
  * Matrices are row-major with contiguous rows and a row stride in elements
  * (ld >= row width).  Any alignment to the element is accepted.  An output
  * must not overlap an input unless said.  Sums, statistics and products
- * accumulate in FP32; BF16 outputs are rounded once, to nearest even.
+ * accumulate in FP32; BF16 outputs are rounded once, to nearest even.  (FP32
+ * products run over three BF16 planes per operand: operands below 2^-110 are
+ * held to 2^-133 there.  Infinities and NaN act as in FP32.)
  * Deterministic: no reduction's order depends on timing.  Every call is
  * asynchronous on the context's stream.  The reverse passes keep partial
  * sums in a workspace of the context (calls on one context that run on

@@ -13,9 +13,9 @@
 //     hold x exactly from 2^-110 up; below, to 2^-133, the smallest bf16
 //     subnormal (the matrix cores keep subnormals).  A product with a value
 //     below 2^-110 is so off by at most 2^-133 times the other operand.  An
-//     infinity or NaN is in the lo plane alone and acts as in FP32; two
-//     infinities that meet give NaN.  Rounded, not cut off: with cut-off
-//     planes mid and lo have the sign of x, and the products that branch.hip
+//     infinity or NaN is in the lo plane, with 1 of its sign in the hi plane,
+//     and acts as in FP32.  Rounded, not cut off: with cut-off planes mid and
+//     lo have the sign of x, and the products that branch.hip
 //     leaves out (mid lo, lo mid, lo lo) shrank every sum by 6e-8 of itself
 //     per layer, which the energies' sums over atoms do not average away;
 //     rounded, they are 6e-9 of either sign.

@@ -41,10 +41,12 @@ __device__ __forceinline__ bf16_t f_to_bf16(float f) {
 
 // The three bf16 planes of an FP32 value (upper 16 bits each), hi and mid
 // rounded to nearest so that what is left has either sign.  A NaN (quiet) or
-// an infinity stands in the lo plane alone, which meets the other operand's hi
-// plane only: a product with a finite value is what FP32 gives.  (In the hi
-// plane an infinity met the other operand's mid and lo planes too, which are 0
-// or of the other sign: NaN.)
+// an infinity stands in the lo plane, which meets the other operand's hi plane
+// only, with 1 of its sign in the hi plane: a product with a finite value, with
+// 0 or with another infinity is what FP32 gives.  (In the hi plane an infinity
+// met the other operand's mid and lo planes too, which are 0 or of the other
+// sign: NaN.  With 0 in the hi plane two infinities met zeros alone: NaN.)
+// Values below 2^-110 are held to 2^-133, the least that a plane holds.
 __device__ __forceinline__ void split3(float x, uint32_t* p) {
   const uint32_t u = __float_as_uint(x);
   const bool fin = (u & 0x7f800000u) != 0x7f800000u;
@@ -53,7 +55,7 @@ __device__ __forceinline__ void split3(float x, uint32_t* p) {
   const float r1 = x - __uint_as_float(h);
   const uint32_t m = (__float_as_uint(r1) + 0x8000u) & 0xffff0000u;
   const float r2 = r1 - __uint_as_float(m);
-  p[0] = fin ? h : 0u;
+  p[0] = fin ? h : (u & 0x80000000u) | 0x3f800000u;
   p[1] = fin ? m : 0u;
   p[2] = fin ? __float_as_uint(r2) & 0xffff0000u
              : (u & 0xffff0000u) | ((u & 0x007fffffu) ? 0x00400000u : 0u);

@@ -144,12 +144,13 @@ hipError_t pack_dense(PrecModel* pm, int prec, const double* W, const double* b,
 }
 
 // The three bf16 planes of an FP32 weight, as split3 forms them (an infinity,
-// from an FP64 weight past FP32's range, in the lo plane).
+// from an FP64 weight past FP32's range, in the lo plane beside 1 in the hi).
 inline void split3_host(float x, uint16_t* hi, uint16_t* mid, uint16_t* lo) {
   uint32_t u;
   memcpy(&u, &x, 4);
   if ((u & 0x7f800000u) == 0x7f800000u) {
-    *hi = *mid = 0;
+    *hi = (uint16_t)((u >> 16 & 0x8000u) | 0x3f80u);
+    *mid = 0;
     *lo = (uint16_t)(u >> 16);
     return;
   }
