@@ -163,17 +163,19 @@ __global__ void __launch_bounds__(TB) k_norm_bwd(long long rows, int cols, const
     }
     float s1 = 0.f, s2 = 0.f;
 #pragma unroll
-    for (int j = 0; j < NJ; ++j)
+    for (int j = 0; j < NJ; ++j) {
+      const int c = (j * LPR + t) * V;
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        // (beyond the row dy is 0, and so is every product with it)
-        h[j][i] = (h[j][i] - mu) * rs;
+        // (0 beyond the row, as dy is: -mu rs may be an infinity)
+        h[j][i] = c + i < cols ? (h[j][i] - mu) * rs : 0.f;
         dg[j][i] += d[j][i] * h[j][i];
         db[j][i] += d[j][i];
         d[j][i] *= g[j][i];
         s1 += d[j][i];
         s2 += d[j][i] * h[j][i];
       }
+    }
     if (dx) {
       s1 = row_sum<LPR>(s1, lds) / width;
       s2 = row_sum<LPR>(s2, lds) / width;
