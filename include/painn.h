@@ -458,7 +458,7 @@ typedef struct {
 } painn_adamw_tensor;
 typedef struct {
   double beta1, beta2;       /* in [0, 1) */
-  double eps;                /* > 0 */
+  double eps;                /* > 0, as an FP32 value too (2^-149 at least) */
   double weight_decay;       /* >= 0 */
   int32_t state_bits;        /* 8 or 32 */
   int32_t grad_precision;    /* PAINN_FP32 or PAINN_BF16 */
@@ -475,10 +475,10 @@ typedef struct painn_adamw painn_adamw;
  * 1024 values), PAINN_E_OOM. */
 painn_status painn_adamw_create(painn_ctx* ctx, int32_t n_tensors, const painn_adamw_tensor* tensors,
                                 const painn_adamw_config* cfg, painn_adamw** out);
-/* One step at learning rate lr (finite, >= 0; else PAINN_E_ARG).  A captured
- * step repeats with the lr and step number of its capture.  After
- * painn_destroy of its context an optimizer refuses every step (PAINN_E_ARG)
- * and can still be freed. */
+/* One step at learning rate lr (>= 0; lr, lr weight_decay and lr / (1 -
+ * beta1^t) finite in FP32; else PAINN_E_ARG).  A captured step repeats with
+ * the lr and step number of its capture.  After painn_destroy of its context
+ * an optimizer refuses every step (PAINN_E_ARG) and can still be freed. */
 painn_status painn_adamw_step(painn_adamw* opt, double lr);
 /* Steps made so far (host). */
 painn_status painn_adamw_steps(const painn_adamw* opt, int64_t* steps);

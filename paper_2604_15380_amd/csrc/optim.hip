@@ -8,6 +8,7 @@
 // all loads first, took 67 us for 10.3 M values and 225 us for 67 M in 8 bits;
 // this takes 57 and 190.  FP32 states pass the caches by, as nothing reads
 // them before the next step: 57 -> 47 us (6.1 TB/s; a 1 GiB copy reaches 5.2).
+#include <float.h>
 #include <math.h>
 
 #include <new>
@@ -165,8 +166,11 @@ __global__ void __launch_bounds__(256) k_adamw(const AdamTensor* __restrict__ te
   }
 }
 
+constexpr int64_t STEPS_MAX = 1LL << 62;
+
 bool in01(double b) { return b >= 0.0 && b < 1.0; }
-bool finite_at_least(double x, double lo) { return x >= lo && x <= 1.7e308; }
+// ... and as an FP32 value, which the kernel has
+bool finite_at_least(double x, double lo) { return x >= lo && x <= FLT_MAX; }
 
 }  // namespace
 
@@ -180,8 +184,8 @@ painn_status painn_adamw_create(painn_ctx* ctx, int32_t n_tensors, const painn_a
     return fail(ctx, PAINN_E_ARG, "null argument or negative tensor count");
   *out = nullptr;
   const painn_adamw_config& c = *cfg;
-  if (!in01(c.beta1) || !in01(c.beta2) || !(c.eps > 0.0) || !finite_at_least(c.eps, 0.0) ||
-      !finite_at_least(c.weight_decay, 0.0) || c.steps < 0)
+  if (!in01(c.beta1) || !in01(c.beta2) || !finite_at_least(c.eps, 0.0) || !((float)c.eps > 0.f) ||
+      !finite_at_least(c.weight_decay, 0.0) || c.steps < 0 || c.steps > STEPS_MAX)
     return fail(ctx, PAINN_E_ARG, "optimizer hyperparameters out of range");
   if (c.state_bits != 8 && c.state_bits != 32) return fail(ctx, PAINN_E_UNSUPPORTED, "state_bits is 8 or 32");
   if (c.grad_precision != PAINN_FP32 && c.grad_precision != PAINN_BF16)
@@ -245,6 +249,9 @@ painn_status painn_adamw_step(painn_adamw* opt, double lr) {
   const AdamScalars s{(float)c.beta1, (float)(1.0 - c.beta1), (float)c.beta2, (float)(1.0 - c.beta2),
                       (float)(1.0 - lr * c.weight_decay), (float)(lr / (1.0 - pow(c.beta1, t))),
                       (float)(1.0 / sqrt(1.0 - pow(c.beta2, t))), (float)c.eps};
+  // (an infinity times the 0 of a value without gradient would be NaN)
+  if (!isfinite(s.keep) || !isfinite(s.step))
+    return fail(ctx, PAINN_E_ARG, "lr is too large for FP32 (lr weight_decay, or lr / (1 - beta1^t))");
   if (opt->chunks) {
     (void)hipSetDevice(ctx->device);
     (void)hipGetLastError();
