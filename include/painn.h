@@ -415,7 +415,9 @@ typedef struct {
 /* args is a host pointer.  Errors: PAINN_E_ARG (null pointers, widths < 1,
  * rows < 0, a stride below the row's width, an unknown activation, dbias
  * without dw), PAINN_E_UNSUPPORTED (FP64; widths above 2^20; more than 2^40
- * rows or 2^31 tiles), PAINN_E_OOM (the reverse pass's workspace). */
+ * rows; a result of 2^24 or more tiles of 128 x 128 values, as one launch
+ * holds no more; 2^34 or more weights in the reverse pass), PAINN_E_OOM (the
+ * reverse pass's workspace). */
 painn_status painn_linear(painn_ctx* ctx, const painn_linear_args* args);
 painn_status painn_linear_backward(painn_ctx* ctx, const painn_linear_backward_args* args);
 
@@ -471,8 +473,8 @@ typedef struct painn_adamw painn_adamw;
  * written in place by every step, and must live as long as the optimizer;
  * states of zeros (8 bits: zero codes and scales) start a run.  Synchronises
  * the stream.  Errors: PAINN_E_ARG (null pointers, values out of range),
- * PAINN_E_UNSUPPORTED (state_bits, grad_precision, more than 2^31 blocks of
- * 1024 values), PAINN_E_OOM. */
+ * PAINN_E_UNSUPPORTED (state_bits, grad_precision, 2^24 blocks of 1024
+ * consecutive values of a tensor or more), PAINN_E_OOM. */
 painn_status painn_adamw_create(painn_ctx* ctx, int32_t n_tensors, const painn_adamw_tensor* tensors,
                                 const painn_adamw_config* cfg, painn_adamw** out);
 /* One step at learning rate lr (>= 0; lr, lr weight_decay and lr / (1 -

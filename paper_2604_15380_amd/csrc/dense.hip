@@ -1049,6 +1049,7 @@ bool launch(hipStream_t st, Args a, long long tiles, long long nt) {
   if (tiles > 0x7fffffffLL / (nt < 8 ? 8 : nt) - 8) return false;
   const long long blocks = (MODE != DW && tiles >= 64 ? ceil_div(tiles, 8) * 8 : tiles) * nt;
   if (blocks == 0) return true;
+  if (blocks > LAUNCH_THREADS / (64 * WM * WN)) return false;
   a.tiles = (int)tiles;
   a.nt = (int)nt;
   a.past = past_caches(a.out, a.ldo, a.gr.rows, sizeof(T));
@@ -1143,6 +1144,8 @@ inline long long dw_chunks(long long rows, long long nt, int groups, bool half) 
   return best;
 }
 
+const char* const TOO_LARGE = "more tiles than a launch of 2^32 threads holds";
+
 template <class T>
 painn_status run_fwd(painn_ctx* ctx, const painn_linear_args& p, int n_groups, const int32_t* offsets) {
   Args a{};
@@ -1158,7 +1161,7 @@ painn_status run_fwd(painn_ctx* ctx, const painn_linear_args& p, int n_groups, c
   prof_mark(ctx->prof, ctx->stream, KC_LINEAR, true);
   const bool ok = run_rows<T, FWD>(ctx->stream, a);
   prof_mark(ctx->prof, ctx->stream, KC_LINEAR, false);
-  if (!ok) return fail(ctx, PAINN_E_UNSUPPORTED, "more than 2^31 tiles");
+  if (!ok) return fail(ctx, PAINN_E_UNSUPPORTED, TOO_LARGE);
   return launched(ctx, "dense layer launch");
 }
 
@@ -1219,6 +1222,7 @@ painn_status run_bwd(painn_ctx* ctx, const painn_linear_backward_args& p, int n_
   const long long chunks = p.rows > 0 ? ceil_div(p.rows, d.chunk) : 1;
   d.tiles = (int)chunks;
   const bool parts = p.dw && chunks > 1;
+  if (parts && ceil_div(wsize, 1024) > LAUNCH_THREADS / 256) return fail(ctx, PAINN_E_UNSUPPORTED, TOO_LARGE);
   const size_t slots = (size_t)(chunks + G - 1);
   const size_t part_bytes = parts ? align256(slots * wsize * sizeof(float)) : 0;
   const size_t need = dz_bytes + zb_bytes + part_bytes + (parts ? slots * p.d_out * sizeof(float) : 0);
@@ -1257,7 +1261,7 @@ painn_status run_bwd(painn_ctx* ctx, const painn_linear_backward_args& p, int n_
     ok = run_rows<T, DX>(st, a);
   }
   prof_mark(ctx->prof, st, KC_LINEAR_BWD, false);
-  if (!ok) return fail(ctx, PAINN_E_UNSUPPORTED, "more than 2^31 tiles");
+  if (!ok) return fail(ctx, PAINN_E_UNSUPPORTED, TOO_LARGE);
   return launched(ctx, "dense layer reverse launch");
 }
 

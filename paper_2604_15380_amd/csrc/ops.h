@@ -29,6 +29,9 @@ inline painn_status launched(painn_ctx* ctx, const char* what) {
   return fail(ctx, PAINN_E_HIP, std::string(what) + ": " + hipGetErrorString(e));
 }
 
+// Threads that one launch holds along an axis of its grid.
+constexpr long long LAUNCH_THREADS = 0xffffffffLL;
+
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // Storage types.  The kernels compute in float.

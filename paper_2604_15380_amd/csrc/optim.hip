@@ -196,9 +196,10 @@ painn_status painn_adamw_create(painn_ctx* ctx, int32_t n_tensors, const painn_a
     if (t.n < 0) return fail(ctx, PAINN_E_ARG, "tensor " + std::to_string(k) + ": negative size");
     if (t.n > 0 && (!t.param || !t.grad || !t.m || !t.v || (c.state_bits == 8 && (!t.m_scale || !t.v_scale))))
       return fail(ctx, PAINN_E_ARG, "tensor " + std::to_string(k) + ": null array");
-    if (t.n > (1LL << 41)) return fail(ctx, PAINN_E_UNSUPPORTED, "more than 2^31 blocks of 1024 values");
-    chunks += (t.n + CHUNK - 1) / CHUNK;
-    if (chunks > 0x7fffffffLL) return fail(ctx, PAINN_E_UNSUPPORTED, "more than 2^31 blocks of 1024 values");
+    constexpr long long most = LAUNCH_THREADS / 256;
+    if (t.n <= most * CHUNK) chunks += (t.n + CHUNK - 1) / CHUNK;
+    if (t.n > most * CHUNK || chunks > most)
+      return fail(ctx, PAINN_E_UNSUPPORTED, "more blocks of 1024 values than a launch holds (2^24 - 1)");
   }
   painn_adamw* o = new (std::nothrow) painn_adamw();
   if (!o) return fail(ctx, PAINN_E_OOM, "host allocation failed");
