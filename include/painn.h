@@ -346,7 +346,8 @@ painn_status painn_trainer_free(painn_trainer* tr);
  * not cols - 1).  gamma, beta [cols] in the precision's type; mean, rstd
  * [rows] FP32 outputs (either may be NULL).  y may be x.
  * Errors: PAINN_E_ARG (null pointers, cols < 1, rows < 0, a stride below
- * cols, eps not finite or < 0), PAINN_E_UNSUPPORTED (FP64). */
+ * cols, eps not finite or < 0), PAINN_E_UNSUPPORTED (FP64; more than 2^30
+ * columns). */
 painn_status painn_layer_norm(painn_ctx* ctx, painn_precision precision, int64_t rows, int32_t cols,
                               const void* x, int64_t ldx, const void* gamma, const void* beta, double eps,
                               void* y, int64_t ldy, float* mean, float* rstd);

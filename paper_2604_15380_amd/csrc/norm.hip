@@ -269,25 +269,29 @@ __global__ void __launch_bounds__(TB) k_norm_cols(long long rows, int cols, cons
   part[((size_t)blockIdx.y * 2 + 1) * cols + c] = db;
 }
 
-// dgamma (blockIdx.y = 0) or dbeta (1): 32 columns per block, the partial rows
-// in 32 slices.
+// dgamma (blockIdx.y = 0) or dbeta (1): 32 columns per block at a time, the
+// partial rows in 32 slices.
 template <class T>
 __global__ void __launch_bounds__(1024) k_norm_fold(int n, int cols, const float* __restrict__ part,
                                                     T* __restrict__ dgamma, T* __restrict__ dbeta) {
   __shared__ float s[32][33];
-  const int q = threadIdx.x >> 5, l = threadIdx.x & 31, c = blockIdx.x * 32 + l;
-  float a = 0.f;
-  if (c < cols) {
+  const int q = threadIdx.x >> 5, l = threadIdx.x & 31;
+  for (int c0 = blockIdx.x * 32; c0 < cols; c0 += gridDim.x * 32) {
+    const int c = c0 + l;
+    float a = 0.f;
+    if (c < cols) {
 #pragma unroll 8
-    for (int k = q; k < n; k += 32) a += part[((size_t)k * 2 + blockIdx.y) * cols + c];
-  }
-  s[q][l] = a;
-  __syncthreads();
-  if (q == 0 && c < cols) {
-    a = 0.f;
+      for (int k = q; k < n; k += 32) a += part[((size_t)k * 2 + blockIdx.y) * cols + c];
+    }
+    s[q][l] = a;
+    __syncthreads();
+    if (q == 0 && c < cols) {
+      a = 0.f;
 #pragma unroll
-    for (int k = 0; k < 32; ++k) a += s[k][l];
-    store<1>((blockIdx.y ? dbeta : dgamma) + c, &a);
+      for (int k = 0; k < 32; ++k) a += s[k][l];
+      store<1>((blockIdx.y ? dbeta : dgamma) + c, &a);
+    }
+    __syncthreads();
   }
 }
 
@@ -305,6 +309,8 @@ struct NormArgs {
 
 constexpr int NORM_GRID = 2048;     // blocks of a launch: 8 per CU
 constexpr int NORM_GRID_BWD = 1024; // and of the reverse pass, whose partial rows are folded
+constexpr int NORM_FOLD = 65536;    // and of that, along the columns
+constexpr int NORM_COLS = 1 << 30;  // a row's columns at most: their count steps by up to 2^21 in an int
 
 inline int grid_for(long long rows, int rpb, int most) {
   const long long n = (rows + rpb - 1) / rpb;
@@ -388,7 +394,8 @@ painn_status run_norm_bwd(const NormArgs& a) {
                                                        (const T*)a.gamma, a.mu, a.rs, (T*)a.dx, a.lddx);
   }
   if (a.dgamma)
-    k_norm_fold<T><<<dim3((c + 31) / 32, 2), 1024, 0, ctx->stream>>>(slices, c, part, (T*)a.dgamma, (T*)a.dbeta);
+    k_norm_fold<T><<<dim3(grid_for(c, 32, NORM_FOLD), 2), 1024, 0, ctx->stream>>>(slices, c, part, (T*)a.dgamma,
+                                                                                (T*)a.dbeta);
   prof_mark(ctx->prof, ctx->stream, KC_NORM_BWD, false);
   return launched(ctx, "layer norm reverse launch");
 }
@@ -398,6 +405,7 @@ painn_status norm_check(painn_ctx* ctx, int prec, int64_t rows, int32_t cols) {
   if (prec != PAINN_FP32 && prec != PAINN_BF16) return fail(ctx, PAINN_E_ARG, "unknown precision");
   if (cols < 1) return fail(ctx, PAINN_E_ARG, "cols must be at least 1");
   if (rows < 0) return fail(ctx, PAINN_E_ARG, "rows must not be negative");
+  if (cols > NORM_COLS) return fail(ctx, PAINN_E_UNSUPPORTED, "more than 2^30 columns");
   return PAINN_OK;
 }
 
