@@ -335,11 +335,11 @@ painn_status painn_trainer_free(painn_trainer* tr);
  * held to 2^-133 there.  Infinities and NaN act as in FP32.)
  * Deterministic: no reduction's order depends on timing.  Every call is
  * asynchronous on the context's stream.  The reverse passes keep partial
- * sums in a workspace of the context (calls on one context that run on
- * different streams must be ordered by the caller); a call that has to enlarge
- * it while the stream is being captured is refused with PAINN_E_OOM (run the
- * call once before the capture, and no larger one while the graph is in
- * use). */
+ * sums in a workspace of the context that only they use (calls on one context
+ * that run on different streams must be ordered by the caller); a call that
+ * has to enlarge it while the stream is being captured is refused with
+ * PAINN_E_OOM (run the call once before the capture, and no larger one while
+ * the graph is in use). */
 
 /* y = (x - mean) rstd gamma + beta for every row of x [rows, cols], mean the
  * row's mean and rstd = 1 / sqrt(variance + eps) (the variance over cols,

@@ -1230,7 +1230,7 @@ painn_status run_bwd(painn_ctx* ctx, const painn_linear_backward_args& p, int n_
     const painn_status ws = ops_workspace(ctx, need);
     if (ws != PAINN_OK) return ws;
   }
-  char* ws = (char*)ctx->bws.p;
+  char* ws = (char*)ctx->ows.p;
   d.part = (float*)(ws + dz_bytes + zb_bytes);
   d.part_b = (float*)(ws + dz_bytes + zb_bytes + part_bytes);
 

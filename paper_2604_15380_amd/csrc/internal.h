@@ -182,6 +182,9 @@ struct painn_ctx {
   Workspace ws;
   // reverse-pass workspace (saved activations and gradients; grown on demand)
   Workspace bws;
+  // partial sums of the head-tuning operators' reverse passes: apart from the
+  // forces', which a captured graph may replay on while those are enlarged
+  Workspace ows;
   // its optimizers (optim.hip): one may outlive the context
   painn_adamw* optimizers = nullptr;
 };

@@ -377,7 +377,7 @@ painn_status run_norm_bwd(const NormArgs& a) {
   if (a.dgamma && slices) {
     const painn_status st = ops_workspace(ctx, (size_t)slices * 2 * c * sizeof(float));
     if (st != PAINN_OK) return st;
-    part = (float*)ctx->bws.p;
+    part = (float*)ctx->ows.p;
   }
   prof_mark(ctx->prof, ctx->stream, KC_NORM_BWD, true);
   if (a.rows > 0 && rpb) {

@@ -8,7 +8,7 @@
 // timing classes, after those of the model's kernels
 enum OpsKernelClass { KC_NORM = KC_COUNT, KC_NORM_BWD, KC_LINEAR, KC_LINEAR_BWD, KC_ADAMW, KC_ALL };
 
-// Room for `need` bytes in the context's reverse-pass workspace.  PAINN_E_OOM
+// Room for `need` bytes in the context's workspace ows.  PAINN_E_OOM
 // where it cannot be had, or only by allocating while the stream is captured.
 painn_status ops_workspace(painn_ctx* ctx, size_t need);
 

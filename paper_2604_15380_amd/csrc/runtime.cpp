@@ -560,6 +560,7 @@ painn_status painn_destroy(painn_ctx* ctx) {
   (void)hipStreamSynchronize(ctx->stream);
   if (ctx->ws.p) (void)hipFree(ctx->ws.p);
   if (ctx->bws.p) (void)hipFree(ctx->bws.p);
+  if (ctx->ows.p) (void)hipFree(ctx->ows.p);
   if (ctx->h_status) (void)hipHostFree(ctx->h_status);
   prof_free(ctx->prof);
   adamw_detach(ctx);
@@ -1300,11 +1301,11 @@ painn_status painn_profile_read(painn_ctx* ctx, int32_t n_max, const char** name
 }  // extern "C"
 
 painn_status ops_workspace(painn_ctx* ctx, size_t need) {
-  if (need <= ctx->bws.bytes) return PAINN_OK;
+  if (need <= ctx->ows.bytes) return PAINN_OK;
   if (capturing(ctx))
     return fail(ctx, PAINN_E_OOM, "the workspace of " + std::to_string(need) +
                                       " bytes is not there and cannot be allocated while the stream is captured");
-  if (!grow_workspace(ctx, ctx->bws, need, need, 8))
+  if (!grow_workspace(ctx, ctx->ows, need, need, 8))
     return fail(ctx, PAINN_E_OOM, "workspace allocation of " + std::to_string(need) + " bytes failed");
   return PAINN_OK;
 }
