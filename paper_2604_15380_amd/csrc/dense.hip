@@ -595,9 +595,10 @@ typedef short s4_t __attribute__((ext_vector_type(4)));
 // (the same for the wave).  Written as an instruction because the compiler
 // would wait for it before any LDS read, the other buffer's too: it knows
 // nothing of it, and wait_loads() does the waiting.  (It has no register
-// output that could be taken too early; m0 has no other use in this file.)
+// output that could be taken too early.  m0, the LDS base, is an operand, which
+// the compiler sets; the instruction needs a cycle after that.)
 __device__ __forceinline__ void load_to_lds(const void* p, uint32_t at) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(p), "s"(at) : "memory");
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(p), "{m0}"(at) : "memory");
 }
 __device__ __forceinline__ uint32_t lds_byte(const void* p) {
   return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
