@@ -344,16 +344,16 @@ painn_status painn_trainer_free(painn_trainer* tr);
 /* y = (x - mean) rstd gamma + beta for every row of x [rows, cols], mean the
  * row's mean and rstd = 1 / sqrt(variance + eps) (the variance over cols,
  * not cols - 1).  gamma, beta [cols] in the precision's type; mean, rstd
- * [rows] FP32 outputs (either may be NULL).  y may be x.
+ * [rows] FP32 outputs (either may be NULL).  y may be x with x's stride.
  * Errors: PAINN_E_ARG (null pointers, cols < 1, rows < 0, a stride below
- * cols, eps not finite or < 0), PAINN_E_UNSUPPORTED (FP64; more than 2^30
+ * cols, another one in place, eps not finite or < 0), PAINN_E_UNSUPPORTED (FP64; more than 2^30
  * columns). */
 painn_status painn_layer_norm(painn_ctx* ctx, painn_precision precision, int64_t rows, int32_t cols,
                               const void* x, int64_t ldx, const void* gamma, const void* beta, double eps,
                               void* y, int64_t ldy, float* mean, float* rstd);
 /* Its reverse pass, from dy = dL/dy and the forward's mean and rstd: dx, and
  * dgamma, dbeta [cols] summed over the rows (zero for no rows).  dx may be
- * NULL (not wanted) or dy; dgamma and dbeta may both be NULL.  Errors as
+ * NULL (not wanted) or dy with dy's stride; dgamma and dbeta may both be NULL.  Errors as
  * painn_layer_norm; PAINN_E_OOM. */
 painn_status painn_layer_norm_backward(painn_ctx* ctx, painn_precision precision, int64_t rows, int32_t cols,
                                        const void* dy, int64_t lddy, const void* x, int64_t ldx,
@@ -414,11 +414,12 @@ typedef struct {
 } painn_linear_backward_args;
 
 /* args is a host pointer.  Errors: PAINN_E_ARG (null pointers, widths < 1,
- * rows < 0, a stride below the row's width, an unknown activation, dbias
- * without dw), PAINN_E_UNSUPPORTED (FP64; widths above 2^20; more than 2^40
- * rows; a result of 2^24 or more tiles of 128 x 128 values, as one launch
- * holds no more; 2^34 or more weights in the reverse pass), PAINN_E_OOM (the
- * reverse pass's workspace). */
+ * rows < 0, a stride below the row's width or another one in place of the
+ * residual or xz, an unknown activation, dbias without dw),
+ * PAINN_E_UNSUPPORTED (FP64; widths above 2^20; more than 2^40 rows; a result
+ * of 2^24 or more tiles of 128 x 128 values, as one launch holds no more; 2^34
+ * or more weights in the reverse pass), PAINN_E_OOM (the reverse pass's
+ * workspace). */
 painn_status painn_linear(painn_ctx* ctx, const painn_linear_args* args);
 painn_status painn_linear_backward(painn_ctx* ctx, const painn_linear_backward_args* args);
 

@@ -1296,6 +1296,8 @@ painn_status fwd_entry(painn_ctx* ctx, const painn_linear_args* p, int n_groups,
   if (!p->x || !p->w || !p->y) return fail(ctx, PAINN_E_ARG, "null array");
   if (p->ldx < p->d_in || p->ldy < p->d_out || (p->residual && p->ldr < p->d_out) || (p->z && p->ldz < p->d_out))
     return fail(ctx, PAINN_E_ARG, "a row stride is below the row's width");
+  if (misplaced(p->y, p->ldy, p->residual, p->ldr, p->rows))
+    return fail(ctx, PAINN_E_ARG, "y in place of the residual has another row stride");
   (void)hipSetDevice(ctx->device);
   (void)hipGetLastError();
   return p->precision == PAINN_FP32 ? run_fwd<float>(ctx, *p, n_groups, offsets)
@@ -1318,6 +1320,8 @@ painn_status bwd_entry(painn_ctx* ctx, const painn_linear_backward_args* p, int 
     if (p->lddy < p->d_out || (p->activation != PAINN_ACT_NONE && p->ldz < p->d_out) || (p->dw && p->ldx < p->d_in) ||
         (p->dx && p->lddx < p->d_in) || (p->dx && p->x_activation != PAINN_ACT_NONE && p->ldxz < p->d_in))
       return fail(ctx, PAINN_E_ARG, "a row stride is below the row's width");
+    if (p->x_activation != PAINN_ACT_NONE && misplaced(p->dx, p->lddx, p->xz, p->ldxz, p->rows))
+      return fail(ctx, PAINN_E_ARG, "dx in place of xz has another row stride");
   }
   if (!p->dw && (!p->dx || p->rows == 0)) return PAINN_OK;
   (void)hipSetDevice(ctx->device);

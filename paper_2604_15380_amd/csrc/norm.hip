@@ -424,6 +424,7 @@ painn_status painn_layer_norm(painn_ctx* ctx, painn_precision precision, int64_t
   if (rows == 0) return PAINN_OK;
   if (!x || !gamma || !beta || !y) return fail(ctx, PAINN_E_ARG, "null array");
   if (ldx < cols || ldy < cols) return fail(ctx, PAINN_E_ARG, "a row stride is below cols");
+  if (misplaced(y, ldy, x, ldx, rows)) return fail(ctx, PAINN_E_ARG, "y in place of x has another row stride");
   (void)hipSetDevice(ctx->device);
   (void)hipGetLastError();
   NormArgs a{};
@@ -444,6 +445,7 @@ painn_status painn_layer_norm_backward(painn_ctx* ctx, painn_precision precision
   if (rows > 0) {
     if (!dy || !x || !gamma || !mean || !rstd) return fail(ctx, PAINN_E_ARG, "null array");
     if (lddy < cols || ldx < cols || (dx && lddx < cols)) return fail(ctx, PAINN_E_ARG, "a row stride is below cols");
+    if (misplaced(dx, lddx, dy, lddy, rows)) return fail(ctx, PAINN_E_ARG, "dx in place of dy has another row stride");
   }
   if (!dgamma && (!dx || rows == 0)) return PAINN_OK;
   (void)hipSetDevice(ctx->device);

@@ -29,6 +29,12 @@ inline painn_status launched(painn_ctx* ctx, const char* what) {
   return fail(ctx, PAINN_E_HIP, std::string(what) + ": " + hipGetErrorString(e));
 }
 
+// Whether an output that may lie in place of an input does so with other rows,
+// which would be overwritten before they are read.
+inline bool misplaced(const void* out, int64_t ldo, const void* in, int64_t ldi, int64_t rows) {
+  return out && out == in && ldo != ldi && rows > 1;
+}
+
 // Threads that one launch holds along an axis of its grid.
 constexpr long long LAUNCH_THREADS = 0xffffffffLL;
 
