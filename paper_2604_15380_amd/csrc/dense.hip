@@ -112,11 +112,14 @@ __device__ __forceinline__ void chunks_of(const Groups& gr, int chunk, int chunk
 // ---- operands -------------------------------------------------------------------
 template <class T> struct Mma;
 template <> struct Mma<b16> {
-  static constexpr int NP = 1, NSUB = 1, BK = 64;
+  static constexpr int NP = 1, BK = 64;
 };
 template <> struct Mma<float> {
-  static constexpr int NP = 3, NSUB = 6, BK = 32;
+  static constexpr int NP = 3, BK = 32;
 };
+// The plane products of FP32, smallest first: lo hi, mid mid, hi lo, mid hi,
+// hi mid, hi hi.
+constexpr int PLANE_A[6] = {2, 1, 0, 1, 0, 0}, PLANE_B[6] = {0, 1, 2, 0, 1, 0};
 
 // An LDS tile is [row][BK] per plane, its 16-byte chunks permuted within the
 // row so that the 16 rows of a fragment, and the rows a transposing store
@@ -544,14 +547,31 @@ __device__ __forceinline__ void product(const Args& g, const Tile<T>& w, uint16_
 #pragma unroll
         for (int p = 0; p < NP; ++p)
           fa[p] = *(const bf8_t*)(As + p * BM * BK + lds_at<BK>(wm + 16 * i + lr, 4 * kk + lq));
-        // smallest products first: lo hi, mid mid, hi lo, mid hi, hi mid, hi hi
-        constexpr int pa[6] = {2, 1, 0, 1, 0, 0}, pb[6] = {0, 1, 2, 0, 1, 0};
+        if constexpr (NP == 3 && MODE != DW) {
+          // A k-block's six products are summed apart and added once: one
+          // rounding of the running sum in place of six.  Error of x w^T at 776
+          // columns 4.2e-7 -> 1.1e-7 (a library's FP32 product 4.9e-7; at dx of
+          // few rows it has 2.5e-7); 65,502 x 776 -> 776 508 -> 516 us, dx 526 ->
+          // 541.  dw's parts per chunk keep its sums short (4,096 rows 2.5e-7,
+          // the library 1.2e-6); apart it took 773 -> 815 us, as its
+          // registers spill.
 #pragma unroll
-        for (int q = 0; q < M::NSUB; ++q)
+          for (int j = 0; j < FN; ++j) {
+            f4_t part = {0, 0, 0, 0};
 #pragma unroll
-          for (int j = 0; j < FN; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j][NP == 1 ? 0 : pb[q]], fa[NP == 1 ? 0 : pa[q]],
-                                                               acc[i][j], 0, 0, 0);
+            for (int q = 0; q < 6; ++q)
+              part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j][PLANE_B[q]], fa[PLANE_A[q]], part, 0, 0, 0);
+            acc[i][j] += part;
+            __builtin_amdgcn_sched_barrier(0);       // (else all six of all j at once: 40 registers more)
+          }
+        } else {
+#pragma unroll
+          for (int q = 0; q < (NP == 1 ? 1 : 6); ++q)
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+              acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j][NP == 1 ? 0 : PLANE_B[q]],
+                                                                 fa[NP == 1 ? 0 : PLANE_A[q]], acc[i][j], 0, 0, 0);
+        }
         if constexpr (MODE == DW)
           if (sum_b) {
             // the column sums of dz, as a product with ones
@@ -829,10 +849,15 @@ __global__ void __launch_bounds__(256) k_few(Args g) {
         bf8_t fa[NP], fb[NP];
         a[i].planes(fa);
         b[i].planes(fb);
-        constexpr int pa6[6] = {2, 1, 0, 1, 0, 0}, pb6[6] = {0, 1, 2, 0, 1, 0};
+        if constexpr (NP == 1) {
+          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[0], fa[0], acc, 0, 0, 0);
+        } else {
+          f4_t part = {0, 0, 0, 0};
 #pragma unroll
-        for (int q = 0; q < M::NSUB; ++q)
-          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[NP == 1 ? 0 : pb6[q]], fa[NP == 1 ? 0 : pa6[q]], acc, 0, 0, 0);
+          for (int q = 0; q < 6; ++q)
+            part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[PLANE_B[q]], fa[PLANE_A[q]], part, 0, 0, 0);
+          acc += part;
+        }
       }
     }
     sums[wave][lane] = acc;
