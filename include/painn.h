@@ -383,6 +383,8 @@ typedef struct {
   int64_t ldy;
   void* z;                   /* [rows, d_out] pre-activations for the reverse pass, or NULL */
   int64_t ldz;
+  int32_t y_fp32;            /* 1: y is FP32 in BF16 too, unrounded, for a readout's few columns; else 0 */
+  int32_t reserved;          /* 0 */
 } painn_linear_args;
 
 /* Its reverse pass: dz = dy activation'(z), dx = dz w, dw = dz^T x, dbias =
@@ -415,7 +417,8 @@ typedef struct {
 
 /* args is a host pointer.  Errors: PAINN_E_ARG (null pointers, widths < 1,
  * rows < 0, a stride below the row's width or another one in place of the
- * residual or xz, an unknown activation, dbias without dw),
+ * residual or xz, FP32 results in place of a BF16 residual, an unknown
+ * activation, dbias without dw),
  * PAINN_E_UNSUPPORTED (FP64; widths above 2^20; more than 2^40 rows; a result
  * of 2^24 or more tiles of 128 x 128 values, as one launch holds no more; 2^34
  * or more weights in the reverse pass), PAINN_E_OOM (the reverse pass's

@@ -286,7 +286,7 @@ class painn_linear_args(ctypes.Structure):
     """include/painn.h painn_linear_args (host struct)."""
     _fields_ = [("precision", _I32), ("activation", _I32), ("rows", _I64), ("d_in", _I32), ("d_out", _I32),
                 ("x", _P), ("ldx", _I64), ("w", _P), ("bias", _P), ("residual", _P), ("ldr", _I64),
-                ("y", _P), ("ldy", _I64), ("z", _P), ("ldz", _I64)]
+                ("y", _P), ("ldy", _I64), ("z", _P), ("ldz", _I64), ("y_fp32", _I32), ("reserved", _I32)]
 
 
 class painn_linear_backward_args(ctypes.Structure):
@@ -299,9 +299,9 @@ class painn_linear_backward_args(ctypes.Structure):
 
 # the same structs from their fields in order, as bytes (null pointers: 0): a
 # quarter of the time that filling a ctypes struct takes
-linear_args = struct.Struct("@iiqiiPqPPPqPqPq").pack
+linear_args = struct.Struct("@iiqiiPqPPPqPqPqii").pack
 linear_backward_args = struct.Struct("@iiqiiPqPqPqPPqiiPqPP").pack
-assert struct.calcsize("@iiqiiPqPPPqPqPq") == ctypes.sizeof(painn_linear_args)
+assert struct.calcsize("@iiqiiPqPPPqPqPqii") == ctypes.sizeof(painn_linear_args)
 assert struct.calcsize("@iiqiiPqPqPqPPqiiPqPP") == ctypes.sizeof(painn_linear_backward_args)
 
 

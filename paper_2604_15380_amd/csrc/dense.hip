@@ -389,7 +389,7 @@ __device__ __forceinline__ void each_tile(const Args& g, Work&& work) {
 // wave's corner in the tile; lds: finish_floats per wave, free for use.
 template <int FN> constexpr int finish_floats() { return 16 * (FN * 16 + 4); }
 
-template <class T, int FM, int FN, int MODE, bool WORDS = false>
+template <class T, class O, int FM, int FN, int MODE, bool WORDS = false>
 __device__ __forceinline__ void finish(const Args& g, const Tile<T>& w, int wm, int wn, const f4_t (&acc)[FM][FN],
                                        const f4_t* accb, bool sum_b, float* lds) {
   constexpr int WT = FN * 16, PITCH = WT + 4, LPR = WT / 8, RPP = 64 / LPR;     // lanes per row, rows per pass
@@ -398,7 +398,7 @@ __device__ __forceinline__ void finish(const Args& g, const Tile<T>& w, int wm, 
   const size_t wsize = (size_t)g.d_out * g.d_in;
   const long long n = w.n0 + wn + (lane % LPR) * 8, left = w.n_end - n;
   const bool whole = MODE != DW || w.slot < 0;
-  T* out = (T*)g.out + (MODE == DW ? (size_t)w.g * wsize : 0) + n;
+  O* out = (O*)g.out + (MODE == DW ? (size_t)w.g * wsize : 0) + n;
   float* part = MODE == DW && !whole ? g.part + (size_t)w.slot * wsize + n : nullptr;
   const long long ldo = MODE == DW ? g.d_in : g.ldo;
   float bias[8];
@@ -490,7 +490,7 @@ __device__ __forceinline__ void finish(const Args& g, const Tile<T>& w, int wm, 
 template <class T, int BM, int BN>
 constexpr int stage_halfs() { return Mma<T>::NP * (BM + BN) * Mma<T>::BK; }
 
-template <class T, int BM, int BN, int WM, int WN, int MODE>
+template <class T, class O, int BM, int BN, int WM, int WN, int MODE>
 __device__ __forceinline__ void product(const Args& g, const Tile<T>& w, uint16_t* lds) {
   using M = Mma<T>;
   constexpr int NP = M::NP, BK = M::BK, TH = 64 * WM * WN;
@@ -583,16 +583,16 @@ __device__ __forceinline__ void product(const Args& g, const Tile<T>& w, uint16_
     }
     __syncthreads();
   }
-  finish<T, FM, FN, MODE>(g, w, wm, wn, acc, accb, sum_b, (float*)lds);
+  finish<T, O, FM, FN, MODE>(g, w, wm, wn, acc, accb, sum_b, (float*)lds);
 }
 
-template <class T, int BM, int BN, int WM, int WN, int MODE>
+template <class T, class O, int BM, int BN, int WM, int WN, int MODE>
 __global__ void __launch_bounds__(64 * WM * WN, 2) k_dense(Args g) {
   constexpr int HALFS = stage_halfs<T, BM, BN>();
   static_assert(HALFS * 2 >= WM * WN * finish_floats<BN / WN / 16>() * 4, "room for finish");
   __shared__ __attribute__((aligned(16))) uint16_t lds[HALFS];
   each_tile<T, BM, BN, MODE>(g, [&](const Tile<T>& w) {
-    product<T, BM, BN, WM, WN, MODE>(g, w, lds);
+    product<T, O, BM, BN, WM, WN, MODE>(g, w, lds);
     if constexpr (MODE == DW) __syncthreads();      // the next group's operands take its place
   });
 }
@@ -692,7 +692,7 @@ struct Dma {
   }
 };
 
-template <int BM, int BN, int WM, int WN, int MODE>
+template <class O, int BM, int BN, int WM, int WN, int MODE>
 __device__ __forceinline__ void product16(const Args& g, const Tile<b16>& w, uint16_t* lds) {
   constexpr int TH = 64 * WM * WN, BK = 64, SA = BM * BK, S = SA + BN * BK;
   constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
@@ -776,16 +776,16 @@ __device__ __forceinline__ void product16(const Args& g, const Tile<b16>& w, uin
     multiply(1);
   }
   __syncthreads();
-  finish<b16, FM, FN, MODE, true>(g, w, wm, wn, acc, accb, sum_b, (float*)lds);
+  finish<b16, O, FM, FN, MODE, true>(g, w, wm, wn, acc, accb, sum_b, (float*)lds);
 }
 
-template <int BM, int BN, int WM, int WN, int MODE>
+template <class O, int BM, int BN, int WM, int WN, int MODE>
 __global__ void __launch_bounds__(64 * WM * WN, 2) k_dense16(Args g) {
   constexpr int HALFS = 2 * (BM + BN) * 64;
   static_assert(HALFS * 2 >= WM * WN * finish_floats<BN / WN / 16>() * 4, "room for finish");
   __shared__ __attribute__((aligned(16))) uint16_t lds[HALFS];
   each_tile<b16, BM, BN, MODE>(g, [&](const Tile<b16>& w) {
-    product16<BM, BN, WM, WN, MODE>(g, w, lds);
+    product16<O, BM, BN, WM, WN, MODE>(g, w, lds);
     if constexpr (MODE == DW) __syncthreads();      // the next group's operands take its place
   });
 }
@@ -824,7 +824,7 @@ struct Words8 {                     // 8 k of one row: 16 or 32 bytes
   }
 };
 
-template <class T>
+template <class T, class O>
 __global__ void __launch_bounds__(256) k_few(Args g) {
   using M = Mma<T>;
   constexpr int NP = M::NP, AHEAD = sizeof(T) == 2 ? 8 : 4;
@@ -879,7 +879,7 @@ __global__ void __launch_bounds__(256) k_few(Args g) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) v[r] += e[r];
       }
-      store_n<4>((T*)g.out + m * g.ldo + c, left, v);
+      store_n<4>((O*)g.out + m * g.ldo + c, left, v);
     }
   });
 }
@@ -1070,7 +1070,7 @@ inline bool past_caches(const void* p, long long ld, long long rows, size_t es) 
   return (uintptr_t)p % 128 == 0 && ld * es % 128 == 0 && rows * ld * es > (32 << 20);
 }
 
-template <class T, int BM, int BN, int WM, int WN, int MODE>
+template <class T, int BM, int BN, int WM, int WN, int MODE, class O = T>
 bool launch(hipStream_t st, Args a, long long tiles, long long nt) {
   if (tiles > 0x7fffffffLL / (nt < 8 ? 8 : nt) - 8) return false;
   const long long blocks = (MODE != DW && tiles >= 64 ? ceil_div(tiles, 8) * 8 : tiles) * nt;
@@ -1078,16 +1078,16 @@ bool launch(hipStream_t st, Args a, long long tiles, long long nt) {
   if (blocks > LAUNCH_THREADS / (64 * WM * WN)) return false;
   a.tiles = (int)tiles;
   a.nt = (int)nt;
-  a.past = past_caches(a.out, a.ldo, a.gr.rows, sizeof(T));
+  a.past = past_caches(a.out, a.ldo, a.gr.rows, sizeof(O));
   a.past_z = past_caches(a.z, a.ldz, a.gr.rows, sizeof(T));
   if constexpr (sizeof(T) == 2) {
     if (words_path<MODE>(a)) {
-      k_dense16<BM, BN, WM, WN, MODE><<<dim3((unsigned)blocks), 64 * WM * WN, 0, st>>>(a);
+      k_dense16<O, BM, BN, WM, WN, MODE><<<dim3((unsigned)blocks), 64 * WM * WN, 0, st>>>(a);
       return true;
     }
   }
   if constexpr (BM > 128 || BN > 128) return false;       // (chosen for words_path only)
-  else k_dense<T, BM, BN, WM, WN, MODE><<<dim3((unsigned)blocks), 64 * WM * WN, 0, st>>>(a);
+  else k_dense<T, O, BM, BN, WM, WN, MODE><<<dim3((unsigned)blocks), 64 * WM * WN, 0, st>>>(a);
   return true;
 }
 
@@ -1106,7 +1106,10 @@ inline long long rounds(const Groups& gr, int bm, int width, int bn, long long a
 // 159 / 171 / 143 (8 / 8.8 / 7); 256 -> 1,024 63 / 67 / 55 (8 / 8.8 / 7); 1,024
 // -> 256 45 / 50 / 40 (2 / 2.5 / 1.7); 256 -> 384, z kept, 33 / 46 / 37 (3 /
 // 3.8 / 3.5).
-template <class T, int MODE>
+// O: the results' type; FP32 from BF16 operands is a readout's form, a few
+// columns wide, and has the small tiles alone (us at 65,502 rows, BF16 results /
+// FP32: 776 -> 1 21.7 / 18.6, 776 -> 776 113 / 218).
+template <class T, int MODE, class O = T>
 bool run_rows(hipStream_t st, const Args& a) {
   const int width = MODE == FWD ? a.d_out : a.d_in;
   const long long rows = tile_bound(a.gr, 128), cols = ceil_div(width, 128);
@@ -1121,13 +1124,16 @@ bool run_rows(hipStream_t st, const Args& a) {
       b.tiles = (int)tile_bound(a.gr, 16);
       b.nt = (int)ceil_div(width, 16);
       const long long blocks = (b.tiles >= 64 ? ceil_div(b.tiles, 8) * 8 : b.tiles) * (long long)b.nt;
-      k_few<T><<<dim3((unsigned)blocks), 256, 0, st>>>(b);
+      k_few<T, O><<<dim3((unsigned)blocks), 256, 0, st>>>(b);
       return true;
     }
   }
-  if (rows * cols < FULL / 2 || (MODE == DX && a.rest))
-    return launch<T, 64, 64, 2, 2, MODE>(st, a, tile_bound(a.gr, 64), ceil_div(width, 64));
-  if constexpr (sizeof(T) == 4) {
+  constexpr bool SMALL = sizeof(O) != sizeof(T);
+  if (SMALL || rows * cols < FULL / 2 || (MODE == DX && a.rest))
+    return launch<T, 64, 64, 2, 2, MODE, O>(st, a, tile_bound(a.gr, 64), ceil_div(width, 64));
+  if constexpr (SMALL) {
+    return false;
+  } else if constexpr (sizeof(T) == 4) {
     // (128 x 128 / 128 x 64: 13,800 rows 337 -> 776 71 / 61 us, its dx 88 / 75; two
     // full rounds, dx of 65,502 x 256 -> 1,024, 212 / 238)
     if (2 * rows * cols <= 3 * FULL) return launch<T, 128, 64, 2, 2, MODE>(st, a, rows, ceil_div(width, 64));
@@ -1141,7 +1147,7 @@ bool run_rows(hipStream_t st, const Args& a) {
       if (c160 < c128) return launch<T, 128, 160, 2, 2, MODE>(st, a, rows, ceil_div(width, 160));
     }
   }
-  return launch<T, 128, 128, 2, 2, MODE>(st, a, rows, cols);
+  if constexpr (!SMALL) return launch<T, 128, 128, 2, 2, MODE>(st, a, rows, cols);
 }
 
 // Chunks of the rows for dw, nt tiles each: of least time, where a k-block
@@ -1185,7 +1191,9 @@ painn_status run_fwd(painn_ctx* ctx, const painn_linear_args& p, int n_groups, c
   a.out = p.y; a.ldo = p.ldy;
   a.z = p.z; a.ldz = p.ldz;
   prof_mark(ctx->prof, ctx->stream, KC_LINEAR, true);
-  const bool ok = run_rows<T, FWD>(ctx->stream, a);
+  bool ok;
+  if constexpr (sizeof(T) == 2) ok = p.y_fp32 ? run_rows<T, FWD, float>(ctx->stream, a) : run_rows<T, FWD>(ctx->stream, a);
+  else ok = run_rows<T, FWD>(ctx->stream, a);
   prof_mark(ctx->prof, ctx->stream, KC_LINEAR, false);
   if (!ok) return fail(ctx, PAINN_E_UNSUPPORTED, TOO_LARGE);
   return launched(ctx, "dense layer launch");
@@ -1321,6 +1329,9 @@ painn_status fwd_entry(painn_ctx* ctx, const painn_linear_args* p, int n_groups,
   if (!p->x || !p->w || !p->y) return fail(ctx, PAINN_E_ARG, "null array");
   if (p->ldx < p->d_in || p->ldy < p->d_out || (p->residual && p->ldr < p->d_out) || (p->z && p->ldz < p->d_out))
     return fail(ctx, PAINN_E_ARG, "a row stride is below the row's width");
+  if (p->y_fp32 != 0 && p->y_fp32 != 1) return fail(ctx, PAINN_E_ARG, "y_fp32 is 0 or 1");
+  if (p->y_fp32 && p->precision == PAINN_BF16 && p->y == p->residual)
+    return fail(ctx, PAINN_E_ARG, "y in place of the residual has another type");
   if (misplaced(p->y, p->ldy, p->residual, p->ldr, p->rows))
     return fail(ctx, PAINN_E_ARG, "y in place of the residual has another row stride");
   (void)hipSetDevice(ctx->device);

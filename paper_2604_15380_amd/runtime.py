@@ -421,6 +421,7 @@ class Runtime:
         return (z if ld == cols else z[:, :cols]), ld
 
     def _dense(self, x, weight, offsets, bias, activation, residual, keep_preact, out):
+        import torch
         prec, t = self._precision(x), x.dtype
         n, i, o, lead, groups, po = self._shapes(x, weight, offsets)
         act = self._activation(activation)
@@ -430,13 +431,14 @@ class Runtime:
         pr, ldr = self._rows(residual, "residual", t, n, o)
         if out is None:
             out = x.new_empty((n, o))
-        py, ldy = self._rows(out, "out", t, n, o)
+        full = out.dtype is torch.float32
+        py, ldy = self._rows(out, "out", torch.float32 if full else t, n, o)
         z, pz, ldz = None, 0, 0
         if keep_preact:
             z, ldz = self._kept(x, n, o)
             pz = z.data_ptr()
         cur = self._enter()
-        a = B.linear_args(prec, act, n, i, o, px, ldx, pw, pb, pr, ldr, py, ldy, pz, ldz)
+        a = B.linear_args(prec, act, n, i, o, px, ldx, pw, pb, pr, ldr, py, ldy, pz, ldz, full, 0)
         if groups:
             B.painn_grouped_linear(self.ctx, a, groups, po)
         else:
@@ -449,7 +451,8 @@ class Runtime:
         """y = activation(x weight^T + bias) + residual; x [rows, d_in], weight
         [d_out, d_in].  keep_preact: (y, z), z the activation's input, for
         linear_backward (a large z has gaps between its rows).  `residual` may
-        be `out`."""
+        be `out`.  A float32 `out` takes a BF16 layer's results unrounded (a
+        readout's, of a few columns)."""
         return self._dense(x, weight, None, bias, activation, residual, keep_preact, out)
 
     def grouped_linear(self, x, weight, offsets, bias=None, activation="none", residual=None, keep_preact=False,

@@ -55,8 +55,8 @@ class HeadTuner:
     """weights: the model's arrays by name (shared{m}.w, shared{m}.b,
     head{h}.{m}.w, head{h}.{m}.b, as the weight file orders them).  F: the
     width of the features.  dtype: "fp32" or "bf16", of the activations, the
-    products' weights and the gradients; masters and sums are FP32, energies
-    FP64.  adapter: the adapter's inner width (0: none).  state_bits: 32 or 8,
+    products' weights and the gradients; masters, sums and atom energies are
+    FP32, energies FP64.  adapter: the adapter's inner width (0: none).  state_bits: 32 or 8,
     of the optimizer's states."""
 
     def __init__(self, rt, weights, F, n_heads, n_shared, n_branch, dtype="bf16", adapter=0, lr=6.34e-4,
@@ -109,7 +109,9 @@ class HeadTuner:
 
     # ---- forward ---------------------------------------------------------
     def _forward(self, b, keep):
-        """Atom energies [N, 1] and what the reverse pass needs of every layer."""
+        """Atom energies [N, 1] in FP32 and what the reverse pass needs of every
+        layer."""
+        import torch
         rt, w, kept = self.rt, self.weight, {}
         a = b["s"]
         if self.adapter:
@@ -126,7 +128,9 @@ class HeadTuner:
         for m in range(self.n_branch):
             last = m + 1 == self.n_branch
             y = rt.grouped_linear(x, w[f"branch{m}.w"], b["offsets"], w[f"branch{m}.b"],
-                                  activation="none" if last else "silu", keep_preact=not last)
+                                  activation="none" if last else "silu", keep_preact=not last,
+                                  out=torch.empty((len(x), 1), dtype=torch.float32, device=x.device)
+                                  if last else None)
             layers.append((f"branch{m}", x, xz))
             x, xz = (y, None) if last else y
         kept["layers"] = layers if keep else None
