@@ -451,8 +451,16 @@ painn_status painn_grouped_linear_backward(painn_ctx* ctx, const painn_linear_ba
  * largest is exact to 2^-4 of itself and values down to 4e-6 of it are kept.
  * A second moment above zero never gets the code of zero: a denominator that
  * vanished beside a first moment that did not would make a step without
- * bound.  The step uses the states before they are coded.  An infinity or NaN
- * in a block's gradients makes the block's states NaN from then on. */
+ * bound.  The step uses the states before they are coded.  Codes are rounded
+ * to nearest at every step, so a value whose step is less than half a code
+ * keeps its code and moves with its block's scale alone, that is with the
+ * block's largest value.  With beta2 = 0.999 that is every sqrt(v) but those
+ * that a gradient 8 times as large meets: after 1,000 steps of gradients of
+ * constant size sqrt(v) lies between 0.55 and 1.95 of what 32 bits hold (0.7 to
+ * 1.5 for nine in ten), and where a value's gradients become small beside its
+ * block's, sqrt(v) stays large and its steps short.  An infinity or NaN in a
+ * block's gradients makes the block's m NaN and its sqrt(v) infinite or NaN
+ * from then on, and so its parameters NaN. */
 typedef struct {
   int64_t n;                 /* values, >= 0 */
   float* param;              /* [n] */
