@@ -14,15 +14,17 @@
 //
 // FP32 operands become three BF16 planes on the way into LDS (split3, mfma.h)
 // and six of the nine plane products are formed: 96 matrix-core cycles per
-// 16x16x32 against 256 of the FP32 instruction, at FP32's accuracy (65,502 x
-// 776 x 776: 0.59 ms, a library's FP32 product 0.79 ms).
+// 16x16x32 against 256 of the FP32 instruction, no further from 64 bits than a
+// plain FP32 product (65,502 x 776 x 776: 0.51 ms, a library's FP32 product
+// 0.72 ms).
 //
-// What bounds it: with BF16 the bytes.  65,536 x 1,024 -> 1,024 takes 131 us, 1.05
-// PFLOP/s (a library's product without epilogue 103); the loads alone take
+// What bounds it: with BF16 the bytes.  65,536 x 1,024 -> 1,024 takes 133 us, 1.03
+// PFLOP/s (a library's product without epilogue 104); the loads alone take
 // 121, the products alone 103.  At 776 columns a row's 128-byte piece lies in
-// two cache lines, which is most of 65,502 x 776 x 776's 110 us (with rows of
-// 832 columns 100).  FP32: the vector instructions that split the planes, 6.6
-// per value, beside 96 matrix instructions per wave and k-block.
+// two cache lines, which is most of 65,502 x 776 x 776's 113 us (with rows of
+// 832 columns 99).  FP32: the vector instructions that split the planes, 6.6
+// per value, beside 96 matrix instructions per wave and k-block; at 65,502 x
+// 776 x 776 the former take 0.50 of the SIMDs' time, the latter 0.46.
 //
 // Rows of a ragged batch are tiled per group: a block finds its tile by a scan
 // over the groups' row counts, one group per lane, so that no launch or

@@ -8,6 +8,8 @@
 // all loads first, took 67 us for 10.3 M values and 225 us for 67 M in 8 bits;
 // this takes 57 and 190.  FP32 states pass the caches by, as nothing reads
 // them before the next step: 57 -> 47 us (6.1 TB/s; a 1 GiB copy reaches 5.2).
+// That is over three sets of arrays in turn, which the last-level cache holds in
+// part; over twelve it is 53 us, 5.4 TB/s.
 #include <float.h>
 #include <math.h>
 

@@ -77,7 +77,9 @@ class AdamW:
     state_bits 8 holds the moments as e4m3 codes of m and sqrt(v) with one
     FP32 scale per 256 values: m[k] and v[k] are then torch.float8_e4m3fn, and
     the values are m[k].float() * m_scale[k] (each scale repeated 256 times)
-    and the square of v[k].float() * v_scale[k]."""
+    and the square of v[k].float() * v_scale[k].  Codes are rounded to nearest,
+    so that over many steps most second moments move with their block only
+    (painn.h has the figures)."""
 
     def __init__(self, rt, params, grads, lr=6.34e-4, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01,
                  state_bits=32, copies=None, state=None, steps=0):
@@ -505,7 +507,9 @@ class Runtime:
         """(dx, dweight, dbias) of linear.  preact: the forward's z, needed with
         an activation.  With x_activation and x_preact (x =
         x_activation(x_preact)), dx is the gradient of x_preact.  The
-        residual's gradient is dy."""
+        residual's gradient is dy.  In BF16 with an activation, dy times its
+        slope is rounded to BF16 before the products where it has more than
+        8,192 values (dbias is not)."""
         return self._dense_backward(dy, x, weight, None, activation, preact, x_activation, x_preact, need_dx, dx,
                                     dweight, dbias)
 

@@ -56,8 +56,8 @@ class HeadTuner:
     head{h}.{m}.w, head{h}.{m}.b, as the weight file orders them).  F: the
     width of the features.  dtype: "fp32" or "bf16", of the activations, the
     products' weights and the gradients; masters, sums and atom energies are
-    FP32, energies FP64.  adapter: the adapter's inner width (0: none).  state_bits: 32 or 8,
-    of the optimizer's states."""
+    FP32, energies FP64.  adapter: the adapter's inner width (0: none).
+    state_bits: 32 or 8, of the optimizer's states."""
 
     def __init__(self, rt, weights, F, n_heads, n_shared, n_branch, dtype="bf16", adapter=0, lr=6.34e-4,
                  betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, state_bits=32, seed=0):
