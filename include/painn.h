@@ -392,8 +392,8 @@ typedef struct {
  * x_activation(xz) came from, dx is the gradient of xz: (dz w)
  * x_activation'(xz), in the same pass.  The residual's gradient is dy.  In
  * BF16 dz is rounded to BF16 before the products where there is an
- * activation and rows * d_out is above 8,192; fewer values are held to 16 bits
- * (a value and its remainder).  relu'(0) = 0. */
+ * activation, rows * d_out is above 8,192 and dz_remainders is 0; else it is
+ * held to 16 bits (a value and its remainder).  relu'(0) = 0. */
 typedef struct {
   int32_t precision, activation;
   int64_t rows;
@@ -408,7 +408,7 @@ typedef struct {
   const void* xz;            /* [rows, d_in]; not read for x_activation PAINN_ACT_NONE */
   int64_t ldxz;
   int32_t x_activation;
-  int32_t reserved;          /* 0 */
+  int32_t dz_remainders;     /* 1: BF16 dz keeps its remainders at any size; else 0 */
   void* dx;                  /* [rows, d_in], or NULL; may be xz with xz's stride */
   int64_t lddx;
   void* dw;                  /* [d_out, d_in], or NULL */
@@ -417,8 +417,8 @@ typedef struct {
 
 /* args is a host pointer.  Errors: PAINN_E_ARG (null pointers, widths < 1,
  * rows < 0, a stride below the row's width or another one in place of the
- * residual or xz, FP32 results in place of a BF16 residual, an unknown
- * activation, dbias without dw),
+ * residual or xz, FP32 results in place of a BF16 residual, y_fp32 or
+ * dz_remainders neither 0 nor 1, an unknown activation, dbias without dw),
  * PAINN_E_UNSUPPORTED (FP64; widths above 2^20; more than 2^40 rows; a result
  * of 2^24 or more tiles of 128 x 128 values, as one launch holds no more; 2^34
  * or more weights in the reverse pass), PAINN_E_OOM (the reverse pass's

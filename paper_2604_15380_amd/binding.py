@@ -293,7 +293,7 @@ class painn_linear_backward_args(ctypes.Structure):
     """include/painn.h painn_linear_backward_args (host struct)."""
     _fields_ = [("precision", _I32), ("activation", _I32), ("rows", _I64), ("d_in", _I32), ("d_out", _I32),
                 ("dy", _P), ("lddy", _I64), ("z", _P), ("ldz", _I64), ("x", _P), ("ldx", _I64), ("w", _P),
-                ("xz", _P), ("ldxz", _I64), ("x_activation", _I32), ("reserved", _I32),
+                ("xz", _P), ("ldxz", _I64), ("x_activation", _I32), ("dz_remainders", _I32),
                 ("dx", _P), ("lddx", _I64), ("dw", _P), ("dbias", _P)]
 
 

@@ -468,7 +468,7 @@ class Runtime:
         return self._dense(x, weight, offsets, bias, activation, residual, keep_preact, out)
 
     def _dense_backward(self, dy, x, weight, offsets, activation, preact, x_activation, x_preact, need_dx, dx,
-                        dweight, dbias):
+                        dweight, dbias, dz_remainders):
         import torch
         prec, t = self._precision(x), x.dtype
         n, i, o, lead, groups, po = self._shapes(x, weight, offsets)
@@ -492,8 +492,8 @@ class Runtime:
         pdw = self._whole(dweight, "dweight", t, lead + (o, i))
         pdb = self._whole(dbias, "dbias", t, lead + (o,))
         cur = self._enter()
-        a = B.linear_backward_args(prec, act, n, i, o, pdy, lddy, pz, ldz, px, ldx, pw, pxz, ldxz, x_act, 0, pdx, lddx,
-                                   pdw, pdb)
+        a = B.linear_backward_args(prec, act, n, i, o, pdy, lddy, pz, ldz, px, ldx, pw, pxz, ldxz, x_act, dz_remainders,
+                                   pdx, lddx, pdw, pdb)
         if groups:
             B.painn_grouped_linear_backward(self.ctx, a, groups, po)
         else:
@@ -503,24 +503,25 @@ class Runtime:
         return dx, dweight, dbias
 
     def linear_backward(self, dy, x, weight, activation="none", preact=None, x_activation="none", x_preact=None,
-                        need_dx=True, dx=None, dweight=None, dbias=None):
+                        need_dx=True, dx=None, dweight=None, dbias=None, dz_remainders=False):
         """(dx, dweight, dbias) of linear.  preact: the forward's z, needed with
         an activation.  With x_activation and x_preact (x =
         x_activation(x_preact)), dx is the gradient of x_preact.  The
         residual's gradient is dy.  In BF16 with an activation, dy times its
         slope is rounded to BF16 before the products where it has more than
-        8,192 values (dbias is not)."""
+        8,192 values (dbias is not); with dz_remainders what that leaves goes
+        through them too, at 2.5 times the time of a large layer."""
         return self._dense_backward(dy, x, weight, None, activation, preact, x_activation, x_preact, need_dx, dx,
-                                    dweight, dbias)
+                                    dweight, dbias, dz_remainders)
 
     def grouped_linear_backward(self, dy, x, weight, offsets, activation="none", preact=None, x_activation="none",
-                                x_preact=None, need_dx=True, dx=None, dweight=None, dbias=None):
+                                x_preact=None, need_dx=True, dx=None, dweight=None, dbias=None, dz_remainders=False):
         """linear_backward of grouped_linear; dweight and dbias of a group
         without rows are zero."""
         if offsets is None:
             raise ValueError("offsets is missing")
         return self._dense_backward(dy, x, weight, offsets, activation, preact, x_activation, x_preact, need_dx, dx,
-                                    dweight, dbias)
+                                    dweight, dbias, dz_remainders)
 
     def adamw(self, params, grads, **how) -> AdamW:
         """An optimizer of these tensors (AdamW's arguments)."""
