@@ -423,7 +423,6 @@ class Runtime:
         return (z if ld == cols else z[:, :cols]), ld
 
     def _dense(self, x, weight, offsets, bias, activation, residual, keep_preact, out):
-        import torch
         prec, t = self._precision(x), x.dtype
         n, i, o, lead, groups, po = self._shapes(x, weight, offsets)
         act = self._activation(activation)
@@ -431,10 +430,10 @@ class Runtime:
         pw = self._whole(weight, "weight", t, lead + (o, i))
         pb = self._whole(bias, "bias", t, lead + (o,))
         pr, ldr = self._rows(residual, "residual", t, n, o)
+        full = out is not None and _precisions().get(out.dtype) == B.PAINN_FP32
         if out is None:
             out = x.new_empty((n, o))
-        full = out.dtype is torch.float32
-        py, ldy = self._rows(out, "out", torch.float32 if full else t, n, o)
+        py, ldy = self._rows(out, "out", out.dtype if full else t, n, o)
         z, pz, ldz = None, 0, 0
         if keep_preact:
             z, ldz = self._kept(x, n, o)
