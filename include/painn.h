@@ -346,8 +346,8 @@ painn_status painn_trainer_free(painn_trainer* tr);
  * not cols - 1).  gamma, beta [cols] in the precision's type; mean, rstd
  * [rows] FP32 outputs (either may be NULL).  y may be x with x's stride.
  * Errors: PAINN_E_ARG (null pointers, cols < 1, rows < 0, a stride below
- * cols, another one in place, eps not finite or < 0), PAINN_E_UNSUPPORTED (FP64; more than 2^30
- * columns). */
+ * cols, another one in place, eps not finite, < 0 or above 0 and 0 in FP32),
+ * PAINN_E_UNSUPPORTED (FP64; more than 2^30 columns). */
 painn_status painn_layer_norm(painn_ctx* ctx, painn_precision precision, int64_t rows, int32_t cols,
                               const void* x, int64_t ldx, const void* gamma, const void* beta, double eps,
                               void* y, int64_t ldy, float* mean, float* rstd);

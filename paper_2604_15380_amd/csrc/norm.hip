@@ -420,7 +420,9 @@ painn_status painn_layer_norm(painn_ctx* ctx, painn_precision precision, int64_t
   ctx->err.clear();
   painn_status st = norm_check(ctx, precision, rows, cols);
   if (st != PAINN_OK) return st;
-  if (!(eps >= 0.0) || !(eps <= 3.4e38)) return fail(ctx, PAINN_E_ARG, "eps must be finite and not negative");
+  // (an eps that is 0 in FP32 alone would make constant rows NaN)
+  if (!(eps >= 0.0) || !(eps <= 3.4e38) || (eps > 0.0 && (float)eps == 0.f))
+    return fail(ctx, PAINN_E_ARG, "eps must be finite and not negative, in FP32 too");
   if (rows == 0) return PAINN_OK;
   if (!x || !gamma || !beta || !y) return fail(ctx, PAINN_E_ARG, "null array");
   if (ldx < cols || ldy < cols) return fail(ctx, PAINN_E_ARG, "a row stride is below cols");

@@ -44,3 +44,19 @@ def test_constant_rows_of_large_values(rt, dtype, cols, eps):
     within(dx.cpu().double() - want, tol, "dx")
     assert not bool(dg.any())
     within(db.cpu().double() - dy.double().sum(0), dy.double().abs().sum(0) * (4 * E32 + half), "db")
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_small_eps(rt, dtype):
+    """An eps above 0 that FP32 holds gives constant rows y = beta; one that it
+    does not is refused."""
+    from paper_2604_15380_amd import PainnError
+    t = DTYPES[dtype]
+    x, g = torch.full((5, 70), 3.0, dtype=t, device="cuda"), torch.ones(70, dtype=t, device="cuda")
+    for eps in (1e-44, 1e-38, 1e-20):
+        y, _, rstd = rt.layer_norm(x, g, g, eps=eps)
+        assert bool((y == 1).all()) and bool(rstd.isfinite().all()), eps
+    for eps in (1e-46, 1e-50, 1e-300):
+        with pytest.raises(PainnError) as e:
+            rt.layer_norm(x, g, g, eps=eps)
+        assert e.value.status == -1
