@@ -1,0 +1,527 @@
+"""Performance cases of further operators for tuning heads in FP32 and BF16:
+group norm with its activation over the rows of ragged samples, the gate that
+sends rows to heads with its balance loss and counts, and the global gradient
+norm over many tensors with clipping, by itself and ahead of the AdamW step.
+
+A pass is one call (a clipped step: two), as a program that tunes heads, an
+adapter or a gate repeats it: rows are atoms or structures, columns are
+features or heads, samples are structures.  Counts and widths are those of
+this repository's workloads (one structure of a relaxation; screening batches
+of about 65,500 atoms in structures of 4 to 200; crystals; the lead model's
+337 features and 16 heads; up to the 64 heads that a model may have) or
+generic.
+"""
+import math
+import random
+
+import torch
+
+own = False
+
+ACTS = ("none", "silu", "relu", "gelu")
+DTYPES = {"fp32": torch.float32, "bf16": torch.bfloat16}
+EPS_NORM = 1e-5
+BALANCE = 0.01                  # the balance loss's coefficient
+LR, BETA1, BETA2, EPS, DECAY = 6.34e-4, 0.9, 0.999, 1e-8, 0.01
+STEPS_DONE = 20                 # optimizer steps before the first pass
+MAX_NORM = 1.0
+
+
+def _norm(name, back, dtype, rows, cols, groups, samples, act="none", ragged=True, hint=False):
+    return {"name": name, "op": "group_norm_backward" if back else "group_norm", "dtype": dtype, "rows": rows,
+            "cols": cols, "groups": groups, "samples": samples, "act": act, "ragged": ragged, "hint": hint}
+
+
+def _gate(name, back, dtype, rows, heads, k, normalize=False, masked=False):
+    return {"name": name, "op": "gate_backward" if back else "gate", "dtype": dtype, "rows": rows, "heads": heads,
+            "k": k, "normalize": normalize, "masked": masked}
+
+
+def _tensors(name, op, grad, heads, d_in, d_hidden, layers, size=20.0):
+    return {"name": name, "op": op, "grad": grad, "heads": heads, "d_in": d_in, "d_hidden": d_hidden, "layers": layers,
+            "norm": size}
+
+
+def listed():
+    return [
+        # one structure of a relaxation, lead-model features: launch-bound
+        _norm("group_norm_one_structure", False, "fp32", 96, 337, 1, 1),
+        # an adapter's normalised SiLU on a screening batch, by structure
+        _norm("group_norm_screening", False, "bf16", 65502, 256, 16, 1871, "silu"),
+        # the same for the reverse pass; the program knows its longest structure
+        _norm("group_norm_backward_screening", True, "bf16", 65502, 256, 16, 1871, "silu", hint=True),
+        # crystals of 1,024 atoms each, FP32
+        _norm("group_norm_crystals", False, "fp32", 147456, 256, 32, 144, "gelu", ragged=False),
+        # a few very large cells
+        _norm("group_norm_backward_cells", True, "fp32", 120000, 192, 8, 5, "silu"),
+        # a small batch's structures over the lead model's 16 heads: latency
+        _gate("gate_small", False, "fp32", 200, 16, 2),
+        # every atom of a screening batch to its two heads
+        _gate("gate_screening", False, "bf16", 65502, 16, 2, normalize=True),
+        # a very large batch of structures over as many heads as a model may have, some masked
+        _gate("gate_backward_wide", True, "fp32", 131072, 64, 4, normalize=True, masked=True),
+        # the reverse pass of a screening batch's gate
+        _gate("gate_backward_screening", True, "bf16", 65502, 16, 2),
+        # a small adapter's gradients, clipped
+        _tensors("clip_adapter", "clip", "fp32", 1, 64, 256, 2),
+        # gradients of many heads in BF16, one tensor per head and layer
+        _tensors("clip_heads", "clip", "bf16", 48, 337, 1024, 2),
+        # an optimizer step of the lead model's heads on clipped gradients
+        _tensors("adamw_clipped_heads", "adamw_clipped", "bf16", 16, 50, 776, 2),
+    ]
+
+
+def _between(rng, lo, hi):
+    return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def draw(rng):
+    kind = rng.choice(["norm", "norm", "norm", "gate", "gate", "clip", "adamw_clipped"])
+    dtype = rng.choice(["fp32", "bf16"])
+    back = rng.random() < 0.5
+    if kind == "norm":
+        groups = _between(rng, 1, 48)
+        cols = groups * _between(rng, 1, max(1, 1024 // groups))
+        rows = _between(rng, 1, min(147456, 30_000_000 // cols))
+        samples = _between(rng, 1, rows)
+        ragged = rng.random() < 0.75
+        c = _norm("", back, dtype, rows if ragged else max(1, rows // samples) * samples, cols, groups, samples,
+                  rng.choice(ACTS), ragged=ragged, hint=rng.random() < 0.3)
+    elif kind == "gate":
+        heads = _between(rng, 1, 256)
+        c = _gate("", back, dtype, _between(rng, 1, min(131072, 8_000_000 // heads)), heads,
+                  rng.randint(1, min(heads, 8)), normalize=rng.random() < 0.5, masked=rng.random() < 0.4)
+    else:
+        c = _tensors("", kind, dtype, _between(rng, 1, 48), _between(rng, 16, 384),
+                     _between(rng, 16, 1024 if kind == "clip" else 512), rng.choice([1, 2]),
+                     rng.choice([0.3, 3.0, 50.0]))
+    del c["name"]
+    return c
+
+
+# --------------------------------------------------------------------------
+# inputs
+# --------------------------------------------------------------------------
+def _device():
+    return torch.device("cuda" if torch.cuda.is_available() else "cpu")
+
+
+def _lengths(case, seed):
+    """Rows per sample.  Structures differ in size by fifty times, and a few
+    have no atom left after a filter.  The sizes belong to the case; the seed
+    says which sample has which."""
+    n, s = case["rows"], case["samples"]
+    if not case["ragged"]:
+        return [n // s] * s
+    fixed = random.Random(n * 131 + s)
+    share = [math.exp(fixed.uniform(0.0, math.log(50.0))) if fixed.random() < 0.98 else 0.0 for _ in range(s)]
+    if not any(share):
+        share[0] = 1.0
+    total = sum(share)
+    sizes = [int(n * k / total) for k in share]
+    kept = [k for k in range(s) if share[k]]
+    for k in range(n - sum(sizes)):
+        sizes[kept[k % len(kept)]] += 1
+    random.Random(seed).shuffle(sizes)
+    return sizes
+
+
+def _tensor_sizes(case):
+    h, i, w = case["heads"], case["d_in"], case["d_hidden"]
+    one = [w * i, w] + [w * w, w] * (case["layers"] - 1) + [w, 1]
+    return one * h
+
+
+def _inputs(case, seed):
+    """Tensors by name, on the GPU."""
+    dev = _device()
+    gen = torch.Generator(device=dev).manual_seed(seed)
+
+    def normal(*shape, scale=1.0, dtype=torch.float32):
+        return (torch.randn(shape, generator=gen, device=dev) * scale).to(dtype)
+
+    if case["op"].startswith("group_norm"):
+        return _norm_inputs(case, seed, normal)
+    if case["op"].startswith("gate"):
+        t, n, h = DTYPES[case["dtype"]], case["rows"], case["heads"]
+        x = normal(n, h, scale=1.5) + normal(h, scale=0.7)      # some heads are favoured
+        if case["masked"]:
+            # heads that a row cannot take, and rows that are padding
+            x[torch.rand(n, h, generator=gen, device=dev) < 0.15] = -math.inf
+            x[torch.rand(n, generator=gen, device=dev) < 0.02] = -math.inf
+        s = {"logits": x.to(t)}
+        if case["op"] == "gate_backward":
+            s["dweights"] = normal(n, case["k"], scale=0.05)
+        return s
+    # gradients (and what a step needs) of all tensors, one behind the other
+    sizes = _tensor_sizes(case)
+    end = sum(sizes)
+    root = case["norm"] / math.sqrt(end)
+    s = {"sizes": sizes, "g": (normal(end) * normal(end, scale=0.7).exp() * (0.5 * root)).to(DTYPES[case["grad"]])}
+    if case["op"] == "adamw_clipped":
+        p = normal(end, scale=0.04)
+        m, v = 0.3 * root * normal(end), (0.2 * root + 0.1 * root * normal(end).abs()) ** 2
+        s.update(p=p, m=m, v=v, copy=p.to(torch.bfloat16), steps=STEPS_DONE)
+    return s
+
+
+def _norm_inputs(case, seed, normal):
+    t, n, c, g = DTYPES[case["dtype"]], case["rows"], case["cols"], case["groups"]
+    sizes = _lengths(case, seed)
+    ids = torch.arange(len(sizes)).repeat_interleave(torch.tensor(sizes)).to(_device())
+    # features whose size and mean differ from structure to structure
+    x = normal(n, c) * normal(len(sizes), 1, scale=0.5).exp()[ids] + normal(len(sizes), 1)[ids]
+    s = {"x": x.to(t), "weight": (1.0 + normal(c, scale=0.1)).to(t), "bias": normal(c, scale=0.1, dtype=t), "ids": ids,
+         "sizes": sizes, "ends": torch.tensor([0] + sizes, dtype=torch.int64).cumsum(0).to(_device())}
+    if case["ragged"]:
+        s["offsets"] = s["ends"].to(torch.int32)
+    if case["op"] == "group_norm_backward":
+        s["dy"] = normal(n, c, scale=0.05, dtype=t)
+        s["mean"], s["rstd"] = _statistics(s["x"].float(), s, g)
+    return s
+
+
+_KEPT = {}
+
+
+def _runtime():
+    """The library context that a program holds from its start."""
+    if "rt" not in _KEPT:
+        from paper_2604_15380_amd import Runtime
+        _KEPT["rt"] = Runtime(0)
+    return _KEPT["rt"]
+
+
+def _cut(a, sizes):
+    return list(a.split(sizes))
+
+
+def prepare(case, seed):
+    s = _inputs(case, seed)
+    s["case"] = case
+    op = case["op"]
+    if op == "clip":
+        s["out"] = torch.empty_like(s["g"])
+    if op == "gate_backward":       # the forward's results are there
+        s.update(_plain_gate({"case": case, "logits": s["logits"]}))
+    if own:
+        rt = _runtime()
+        if op.startswith("group_norm"):
+            s["how"] = dict(activation=case["act"])
+            if case["ragged"]:
+                s["how"]["offsets"] = s["offsets"]
+                if case["hint"]:
+                    s["how"]["max_rows"] = max(s["sizes"])
+            else:
+                s["how"]["sample_rows"] = case["rows"] // case["samples"]
+        elif op == "gate_backward":
+            s["gate"] = rt.gate(s["logits"], case["k"], normalize=case["normalize"])
+        elif op == "clip":          # a program makes its tables once
+            s["clip"] = rt.grad_norm(_cut(s["g"], s["sizes"]), outs=_cut(s["out"], s["sizes"]))
+        elif op == "adamw_clipped":
+            cut = lambda k: _cut(s[k], s["sizes"])  # noqa: E731
+            s["clip"] = rt.grad_norm(cut("g"))
+            s["optimizer"] = rt.adamw(cut("p"), cut("g"), lr=LR, betas=(BETA1, BETA2), eps=EPS, weight_decay=DECAY,
+                                      copies=cut("copy"), steps=s["steps"], state=dict(m=cut("m"), v=cut("v")))
+    return s
+
+
+# --------------------------------------------------------------------------
+# a pass
+# --------------------------------------------------------------------------
+def run(s):
+    return (_own if own else _plain)[s["case"]["op"]](s)
+
+
+def _own_norm(s):
+    y, mean, rstd = _runtime().group_norm(s["x"], s["weight"], s["bias"], s["case"]["groups"], eps=EPS_NORM, **s["how"])
+    return {"y": y, "mean": mean, "rstd": rstd}
+
+
+def _own_norm_backward(s):
+    dx, dw, db = _runtime().group_norm_backward(s["dy"], s["x"], s["weight"], s["bias"], s["mean"], s["rstd"],
+                                                s["case"]["groups"], **s["how"])
+    return {"dx": dx, "dweight": dw, "dbias": db}
+
+
+def _own_gate(s):
+    g = _runtime().gate(s["logits"], s["case"]["k"], normalize=s["case"]["normalize"])
+    return {"weights": g.weights, "indices": g.indices, "counts": g.counts, "share": g.share, "loss": g.loss}
+
+
+def _own_gate_backward(s):
+    return {"dlogits": _runtime().gate_backward(s["dweights"], s["logits"], s["gate"], balance=BALANCE)}
+
+
+def _own_clip(s):
+    return {"out": s["out"], "norm": s["clip"].clip(MAX_NORM)}
+
+
+def _own_adamw(s):
+    norm, factor = s["clip"].compute(MAX_NORM)
+    s["optimizer"].step(grad_scale=factor)
+    return {"norm": norm, **{k: s[k] for k in ("p", "m", "v", "copy")}}
+
+
+def _act(z, kind):
+    if kind == "silu":
+        return z / (1.0 + torch.exp(-z))
+    if kind == "relu":
+        return z.clamp_min(0.0)
+    if kind == "gelu":
+        return 0.5 * z * (1.0 + torch.erf(z * math.sqrt(0.5)))
+    return z
+
+
+def _act_slope(z, kind):
+    if kind == "none":
+        return torch.ones_like(z)
+    if kind == "silu":
+        t = 1.0 / (1.0 + torch.exp(-z))
+        return t * (1.0 + z * (1.0 - t))
+    if kind == "relu":
+        return (z > 0).to(z.dtype)
+    return 0.5 * (1.0 + torch.erf(z * math.sqrt(0.5))) + z * torch.exp(-0.5 * z * z) * (1 / math.sqrt(2 * math.pi))
+
+
+def _means(a, s):
+    """Means over every sample's rows and group's columns: a [rows, groups,
+    columns of a group]; 0 for a sample without rows."""
+    run = a.sum(2).double().t().contiguous().cumsum(1)
+    run = torch.cat([torch.zeros_like(run[:, :1]), run], 1)
+    total = run[:, s["ends"][1:]] - run[:, s["ends"][:-1]]
+    count = (s["ends"][1:] - s["ends"][:-1]).clamp_min(1) * a.shape[2]
+    return (total / count).t().float()
+
+
+def _statistics(x, s, groups):
+    """mean and rstd [samples, groups]; both 0 for a sample without rows."""
+    x = x.view(len(x), groups, -1)
+    mean = _means(x, s)
+    d = x - mean[s["ids"]][:, :, None]
+    rstd = 1.0 / torch.sqrt(_means(d * d, s) + EPS_NORM)
+    some = s["ends"][1:] > s["ends"][:-1]
+    return mean, torch.where(some[:, None], rstd, torch.zeros_like(rstd))
+
+
+def _plain_norm(s):
+    c = s["case"]
+    x = s["x"].float()
+    mean, rstd = _statistics(x, s, c["groups"])
+    h = (x.view(len(x), c["groups"], -1) - mean[s["ids"]][:, :, None]) * rstd[s["ids"]][:, :, None]
+    y = _act(h.reshape(x.shape) * s["weight"].float() + s["bias"].float(), c["act"])
+    return {"y": y.to(s["x"].dtype), "mean": mean, "rstd": rstd}
+
+
+def _plain_norm_backward(s):
+    c, t = s["case"], s["x"].dtype
+    shape = (len(s["x"]), c["groups"], -1)
+    w, rstd = s["weight"].float(), s["rstd"][s["ids"]][:, :, None]
+    xh = (s["x"].float().view(shape) - s["mean"][s["ids"]][:, :, None]) * rstd
+    flat = xh.reshape(s["x"].shape)
+    dz = s["dy"].float() * _act_slope(flat * w + s["bias"].float(), c["act"])
+    a = (dz * w).view(shape)
+    dx = rstd * (a - _means(a, s)[s["ids"]][:, :, None] - xh * _means(a * xh, s)[s["ids"]][:, :, None])
+    return {"dx": dx.reshape(flat.shape).to(t), "dweight": (dz * flat).sum(0, dtype=torch.float64).to(t),
+            "dbias": dz.sum(0, dtype=torch.float64).to(t)}
+
+
+def _softmax(x):
+    """Softmax over the heads; zeros for a row that can take none."""
+    top = x.amax(1, keepdim=True)
+    some = top > -math.inf
+    e = torch.exp(x - torch.where(some, top, torch.zeros_like(top)))
+    return torch.where(some, e / e.sum(1, keepdim=True), torch.zeros_like(e)), some[:, 0]
+
+
+def _plain_gate(s):
+    c, x = s["case"], s["logits"].float()
+    p, some = _softmax(x)
+    order = torch.sort(x, dim=1, descending=True, stable=True).indices[:, :c["k"]]
+    taken = x.gather(1, order) > -math.inf
+    w = torch.where(taken, p.gather(1, order), torch.zeros_like(p[:, :1]))
+    if c["normalize"]:
+        total = w.sum(1, keepdim=True)
+        w = w / torch.where(total > 0, total, torch.ones_like(total))
+    heads = torch.where(taken, order, torch.full_like(order, -1))
+    counts = (heads[:, :, None] == torch.arange(c["heads"], device=x.device)).sum((0, 1))
+    rows = some.sum().clamp_min(1)
+    share = (p.sum(0, dtype=torch.float64) / rows).float()
+    loss = c["heads"] * (counts.double() / counts.sum().clamp_min(1) * share).sum()
+    return {"weights": w, "indices": heads.to(torch.int32), "counts": counts.to(torch.int32), "share": share,
+            "loss": loss.float()}
+
+
+def _plain_gate_backward(s):
+    c, x = s["case"], s["logits"].float()
+    p, some = _softmax(x)
+    heads, taken = s["indices"].long(), s["indices"] >= 0
+    dw = torch.where(taken, s["dweights"], torch.zeros_like(s["dweights"]))
+    at = heads.clamp_min(0)
+    f = s["counts"].double() / s["counts"].sum().clamp_min(1)
+    dp = (f * (BALANCE * c["heads"] / some.sum().clamp_min(1))).float()
+    dx = p * (dp - (p * dp).sum(1, keepdim=True))
+    w = s["weights"]
+    if c["normalize"]:      # the chosen heads' own softmax
+        dx = dx.scatter_add(1, at, w * (dw - (w * dw).sum(1, keepdim=True)))
+    else:
+        dot = (w * dw).sum(1, keepdim=True)
+        dx = (dx - p * dot).scatter_add(1, at, w * dw)
+    return {"dlogits": dx.to(s["logits"].dtype)}
+
+
+def _factor(norm):
+    return torch.where(norm > MAX_NORM, MAX_NORM / norm, torch.ones_like(norm)).float()
+
+
+def _plain_clip(s):
+    g = s["g"].float()
+    norm = torch.sqrt((g.double() * g.double()).sum())
+    return {"out": (g * _factor(norm)).to(s["g"].dtype), "norm": norm.float()}
+
+
+def _plain_adamw(s):
+    g = s["g"].float()
+    norm = torch.sqrt((g.double() * g.double()).sum())
+    g = g * _factor(norm)
+    s["steps"] += 1
+    m = s["m"] * BETA1 + g * (1.0 - BETA1)
+    v = s["v"] * BETA2 + (g * g) * (1.0 - BETA2)
+    step = LR / (1.0 - BETA1 ** s["steps"])
+    down = 1.0 / math.sqrt(1.0 - BETA2 ** s["steps"])
+    s["p"] = s["p"] * (1.0 - LR * DECAY) - (m * step) / (torch.sqrt(v) * down + EPS)
+    s["m"], s["v"], s["copy"] = m, v, s["p"].to(torch.bfloat16)
+    return {"norm": norm.float(), **{k: s[k] for k in ("p", "m", "v", "copy")}}
+
+
+_plain = {"group_norm": _plain_norm, "group_norm_backward": _plain_norm_backward, "gate": _plain_gate,
+          "gate_backward": _plain_gate_backward, "clip": _plain_clip, "adamw_clipped": _plain_adamw}
+_own = {"group_norm": _own_norm, "group_norm_backward": _own_norm_backward, "gate": _own_gate,
+        "gate_backward": _own_gate_backward, "clip": _own_clip, "adamw_clipped": _own_adamw}
+
+
+# --------------------------------------------------------------------------
+# what a pass cannot do without, and its outputs in 64 bits
+# --------------------------------------------------------------------------
+def work(case):
+    if case["op"] in ("clip", "adamw_clipped"):
+        n, es = sum(_tensor_sizes(case)), 2 if case["grad"] == "bf16" else 4
+        if case["op"] == "clip":
+            return {"bytes": 2 * n * es, "flops": 3 * n}
+        return {"bytes": n * (es + 24 + 2), "flops": 17 * n}
+    es, n = 2 if case["dtype"] == "bf16" else 4, case["rows"]
+    if case["op"].startswith("gate"):
+        h, k = case["heads"], case["k"]
+        if case["op"] == "gate":
+            return {"bytes": es * n * h + 8 * n * k + 8 * h, "flops": n * h * (6 + k)}
+        return {"bytes": 2 * es * n * h + n * k * (12 if case["normalize"] else 8) + 4 * h, "flops": n * h * 9}
+    c, stats = case["cols"], 8 * case["samples"] * case["groups"]
+    if case["op"] == "group_norm":
+        return {"bytes": es * (2 * n * c + 2 * c) + stats, "flops": 9 * n * c}
+    return {"bytes": es * (3 * n * c + 4 * c) + stats, "flops": 18 * n * c}
+
+
+def exact(case, seed):
+    s = _inputs(case, seed)
+    op = case["op"]
+    if op.startswith("group_norm"):
+        return _exact_norm(case, s)
+    if op.startswith("gate"):
+        return _exact_gate(case, s)
+    g = s["g"].double()
+    norm = torch.linalg.vector_norm(g)
+    g = g * min(1.0, MAX_NORM / float(norm))
+    if op == "clip":
+        return {"out": g, "norm": norm}
+    t = s["steps"] + 1
+    m, v = torch.lerp(g, s["m"].double(), BETA1), torch.lerp(g ** 2, s["v"].double(), BETA2)
+    p = s["p"].double()
+    p = p - LR * DECAY * p - LR * (m / (1 - BETA1 ** t)) / ((v / (1 - BETA2 ** t)).sqrt() + EPS)
+    return {"norm": norm, "p": p, "m": m, "v": v, "copy": p}
+
+
+_FN = {"none": lambda z: z, "silu": torch.nn.functional.silu, "relu": torch.nn.functional.relu,
+       "gelu": torch.nn.functional.gelu}
+
+
+def _exact_norm(case, s):
+    """Sample by sample; many short samples as one padded array."""
+    dev, g, c = s["x"].device, case["groups"], case["cols"]
+    sizes = s["sizes"]
+    x, w, b = s["x"].double(), s["weight"].double(), s["bias"].double()
+    back = case["op"] == "group_norm_backward"
+    starts = [0]
+    for k in sizes:
+        starts.append(starts[-1] + k)
+    mean = torch.zeros(len(sizes), g, dtype=torch.float64, device=dev)
+    rstd = torch.zeros_like(mean)
+    out = torch.empty_like(x)
+    dw, db = torch.zeros_like(w), torch.zeros_like(b)
+    order = sorted((k for k in range(len(sizes)) if sizes[k]), key=lambda k: sizes[k])
+    first = 0
+    while first < len(order):
+        # a lot: samples in the order of their lengths, at most 4 M padded values
+        last = first + 1
+        while last < len(order) and (last + 1 - first) * sizes[order[last]] * c <= 4_000_000:
+            last += 1
+        lot = order[first:last]
+        first = last
+        at = torch.tensor([starts[k] for k in lot], device=dev)
+        n = torch.tensor([sizes[k] for k in lot], device=dev)
+        place = torch.arange(sizes[lot[-1]], device=dev)
+        here = place < n[:, None]
+        rows = torch.where(here, at[:, None] + place, torch.zeros_like(place))
+        on = here[:, :, None, None].double()
+        v = x[rows].view(len(lot), -1, g, c // g)
+        lot = torch.tensor(lot, device=dev)
+        each = (n * (c // g))[:, None].double()
+        if not back:
+            mu = (v * on).sum((1, 3)) / each
+            r = ((((v - mu[:, None, :, None]) * on) ** 2).sum((1, 3)) / each + EPS_NORM).rsqrt()
+            mean[lot], rstd[lot] = mu, r
+            h = (v - mu[:, None, :, None]) * r[:, None, :, None]
+            y = _FN[case["act"]](h.flatten(2) * w + b)
+            out[rows[here]] = y[here]
+            continue
+        mu, r = s["mean"][lot].double()[:, None, :, None], s["rstd"][lot].double()[:, None, :, None]
+        h = (v - mu) * r
+        z = (h.flatten(2) * w + b).requires_grad_(True)
+        slope = torch.autograd.grad(_FN[case["act"]](z).sum(), z)[0]
+        dz = s["dy"].double()[rows] * slope * here[:, :, None]
+        dw += (dz * h.flatten(2)).sum((0, 1))
+        db += dz.sum((0, 1))
+        up = (dz * w).view_as(v)
+        # off the set's ones and off x - mean
+        dx = r * (up - (up.sum((1, 3)) / each)[:, None, :, None]
+                  - h * ((up * h).sum((1, 3)) / each)[:, None, :, None])
+        out[rows[here]] = dx.flatten(2)[here]
+    return {"dx": out, "dweight": dw, "dbias": db} if back else {"y": out, "mean": mean, "rstd": rstd}
+
+
+def _exact_gate(case, s):
+    x, h, k = s["logits"].double(), case["heads"], case["k"]
+    some = (x > -math.inf).any(1)
+    # a head's place: how many come before it, the lower head first among equals
+    place = torch.zeros(x.shape, dtype=torch.int64, device=x.device)
+    for j in range(h):
+        other = x[:, j:j + 1]
+        place += (other > x) | ((other == x) & (torch.arange(h, device=x.device) > j))
+    chosen = (place < k) & (x > -math.inf)
+    safe = torch.where(some[:, None], x, torch.zeros_like(x)).requires_grad_(True)
+    p = torch.softmax(safe, 1) * some[:, None]
+    counts = chosen.sum(0)
+    rows = some.sum().clamp_min(1)
+    share = p.sum(0) / rows
+    loss = h * (counts / counts.sum().clamp_min(1) * share).sum()
+    heads = torch.full((len(x), k + 1), -1, dtype=torch.int64, device=x.device)
+    heads.scatter_(1, torch.where(chosen, place, torch.full_like(place, k)),
+                   torch.arange(h, device=x.device).expand(len(x), h))
+    heads = heads[:, :k]
+    w = p.gather(1, heads.clamp_min(0)) * (heads >= 0)
+    if case["normalize"]:
+        w = w / torch.where(some, w.sum(1), torch.ones_like(p[:, 0]))[:, None]
+    if case["op"] == "gate":
+        return {"weights": w.detach(), "indices": heads.to(torch.int32), "counts": counts.to(torch.int32),
+                "share": share.detach(), "loss": loss.detach()}
+    total = (w * s["dweights"].double()).sum() + BALANCE * loss
+    return {"dlogits": torch.autograd.grad(total, safe)[0] * some[:, None]}
