@@ -414,7 +414,7 @@ def work(case):
         h, k = case["heads"], case["k"]
         if case["op"] == "gate":
             return {"bytes": es * n * h + 8 * n * k + 8 * h, "flops": n * h * (6 + k)}
-        return {"bytes": 2 * es * n * h + n * k * (12 if case["normalize"] else 8) + 4 * h, "flops": n * h * 9}
+        return {"bytes": 2 * es * n * h + 8 * n * k + 4 * h, "flops": n * h * 9}
     c, stats = case["cols"], 8 * case["samples"] * case["groups"]
     if case["op"] == "group_norm":
         return {"bytes": es * (2 * n * c + 2 * c) + stats, "flops": 9 * n * c}
