@@ -322,9 +322,10 @@ painn_status painn_trainer_free(painn_trainer* tr);
 /* The operators that a program needs to tune heads or an adapter in FP32 or
  * BF16 on the features of an encoder that stays as it is (section
  * "Precision-sensitivity characterization at inference and fine-tuning
- * stage"): layer norm, the dense layer with its epilogue, the dense layer
- * grouped by dataset head, each with its reverse pass, and AdamW over many
- * tensors.  FP64 is refused (PAINN_E_UNSUPPORTED): painn_trainer_* trains
+ * stage"): layer norm, group norm over a structure's rows, the dense layer
+ * with its epilogue, the dense layer grouped by dataset head, the gate over
+ * the heads with its balance loss, each with its reverse pass, and the global
+ * gradient norm and AdamW over many tensors.  FP64 is refused (PAINN_E_UNSUPPORTED): painn_trainer_* trains
  * whole models in FP64.
  *
  * Matrices are row-major with contiguous rows and a row stride in elements
@@ -366,6 +367,55 @@ typedef enum {
   PAINN_ACT_RELU = 2,        /* max(z, 0) */
   PAINN_ACT_GELU = 3         /* z (1 + erf(z / sqrt 2)) / 2 */
 } painn_activation;
+
+/* Group norm with an activation, channels last: rows are the points of samples
+ * (a structure's atoms), columns fall into `groups` equal groups, and a
+ * sample's rows times a group's columns have one mean and one variance:
+ *   y = activation((x - mean) rstd gamma + beta),  rstd = 1 / sqrt(variance + eps)
+ * (the variance over all values of the set).  Sample s has the rows
+ * [offsets[s], offsets[s+1]) (offsets [n_samples + 1] int32, device,
+ * non-decreasing within [0, rows]; entries outside are taken as the nearest
+ * bound), or with offsets NULL [s sample_rows, (s+1) sample_rows), rows =
+ * n_samples sample_rows.  A sample may be empty: its mean and rstd are 0.  Rows
+ * of no sample are not written.  The sums of a set are formed in FP64 (forward)
+ * or in FP32 for a few rows and FP64 beyond (reverse). */
+typedef struct {
+  int32_t precision, activation;
+  int64_t rows;
+  int32_t cols, groups;
+  const int32_t* offsets;    /* [n_samples + 1], or NULL */
+  int64_t sample_rows;       /* without offsets */
+  int32_t n_samples, reserved;
+  int64_t max_rows;          /* no sample has more rows; 0: not known.  Saves a launch; a longer one is still right */
+  double eps;                /* (forward) */
+  const void* x;             /* [rows, cols] */
+  int64_t ldx;
+  const void* gamma;         /* [cols] */
+  const void* beta;          /* [cols] */
+  void* y;                   /* [rows, cols]; may be x with x's stride (forward) */
+  int64_t ldy;
+  float* mean;               /* [n_samples, groups]: written by the forward (or NULL), read by the reverse pass */
+  float* rstd;
+  void* workspace;           /* device, painn_group_norm_workspace bytes, 16-byte aligned */
+  int64_t workspace_bytes;
+} painn_group_norm_args;
+/* Bytes of workspace for a call of these sizes (sample_rows 0: with offsets). */
+int64_t painn_group_norm_workspace(painn_precision precision, int64_t rows, int32_t cols, int32_t groups,
+                                   int32_t n_samples, int64_t sample_rows, int64_t max_rows, int32_t backward);
+/* args is a host pointer.  Errors: PAINN_E_ARG (null pointers, counts < 0,
+ * groups that do not divide cols, rows that are not n_samples sample_rows
+ * without offsets, a stride below cols or another one in place, an unknown
+ * activation, eps as in painn_layer_norm, reserved not 0, a workspace that is
+ * too small), PAINN_E_UNSUPPORTED (FP64; more than 4096 columns in a group,
+ * 2^24 columns or 2^31 - 1 rows; more blocks than a launch holds). */
+painn_status painn_group_norm(painn_ctx* ctx, const painn_group_norm_args* args);
+/* Its reverse pass, from dy = dL/dy and the forward's x, mean and rstd (y is
+ * not read): dx, and dgamma, dbeta [cols] summed over the samples' rows (zero
+ * for none).  dx may be NULL (not wanted) or dy with dy's stride; dgamma and
+ * dbeta may both be NULL.  The pre-activations are formed again from x.
+ * Errors as painn_group_norm. */
+painn_status painn_group_norm_backward(painn_ctx* ctx, const painn_group_norm_args* args, const void* dy, int64_t lddy,
+                                       void* dx, int64_t lddx, void* dgamma, void* dbeta);
 
 /* A dense layer: z = x w^T + bias, y = activation(z) + residual. */
 typedef struct {
@@ -438,6 +488,80 @@ painn_status painn_grouped_linear(painn_ctx* ctx, const painn_linear_args* args,
 painn_status painn_grouped_linear_backward(painn_ctx* ctx, const painn_linear_backward_args* args,
                                            int32_t n_groups, const int32_t* offsets);
 
+/* The gate over the heads: each row's softmax, its k largest heads, the heads'
+ * counts and the balance loss that keeps a gate from sending every row to the
+ * same few heads.  With p the softmax of a row's logits,
+ *   indices: the heads of the k largest logits, the largest first, ties to the
+ *     lowest head; weights: their p, or with normalize p / (sum of the chosen p);
+ *   counts[h]: how often head h was chosen; share[h]: the mean of p over the
+ *     rows that have a head;
+ *   loss = heads sum_h (counts[h] / sum counts) share[h]  (1 when balanced).
+ * A logit of -infinity is a head that the row cannot take: its p is 0, and it
+ * is never chosen; places without a head have index -1 and weight 0.  A row of
+ * none has no part in share and loss.  NaN counts as the largest logit and
+ * makes its row's weights, share and loss NaN, as +infinity does. */
+typedef struct {
+  int32_t precision;         /* of the logits: PAINN_FP32 or PAINN_BF16 */
+  int32_t heads;
+  int64_t rows;
+  int32_t k, normalize;      /* 1 <= k <= heads; 0 or 1 */
+  const void* logits;        /* [rows, heads] */
+  int64_t ldx;
+  float* weights;            /* [rows, k] (forward) */
+  int32_t* indices;          /* [rows, k]: written by the forward, read by the reverse pass */
+  int32_t* counts;           /* [heads + 1], the last: rows that have a head; written, then read */
+  float* share;              /* [heads] (forward) */
+  float* loss;               /* [1] (forward) */
+  void* workspace;           /* device, painn_gate_workspace bytes, 16-byte aligned (forward) */
+  int64_t workspace_bytes;
+} painn_gate_args;
+/* Bytes of workspace for a forward of these sizes. */
+int64_t painn_gate_workspace(painn_precision precision, int64_t rows, int32_t heads, int32_t k);
+/* args is a host pointer.  Errors: PAINN_E_ARG (null pointers, rows < 0, k
+ * outside [1, heads], a stride below heads, normalize neither 0 nor 1, a
+ * workspace that is too small), PAINN_E_UNSUPPORTED (FP64; more than 1024
+ * heads; 2^31 or more choices). */
+painn_status painn_gate(painn_ctx* ctx, const painn_gate_args* args);
+/* Its reverse pass: dlogits of (sum dweights weights) + balance loss, from the
+ * forward's logits, indices and counts (the counts are constants of the loss).
+ * dweights [rows, k] FP32, or NULL (zero); its values at places without a head
+ * are not used.  Masked logits get 0.  dlogits may be the logits with their
+ * stride.  Errors as painn_gate, and PAINN_E_ARG for another stride in place or a
+ * balance that is not finite in FP32. */
+painn_status painn_gate_backward(painn_ctx* ctx, const painn_gate_args* args, const float* dweights, double balance,
+                                 void* dlogits, int64_t ldd);
+
+/* The global norm of many tensors' gradients, and clipping: norm = the square
+ * root of the sum of all squares (in FP64), factor = max_norm / norm where the
+ * norm is above max_norm, else 1; clipped gradients are g factor.  A norm of
+ * infinity has the factor 0 (which makes infinite gradients NaN), a norm of NaN
+ * the factor NaN. */
+typedef struct {
+  int64_t n;                 /* values, >= 0 */
+  const void* grad;          /* [n] */
+  void* out;                 /* [n] of the same type: where painn_grad_norm_clip writes; may be grad; or NULL */
+  int32_t precision;         /* PAINN_FP32 or PAINN_BF16 */
+  int32_t reserved;          /* 0 */
+} painn_grad_tensor;
+typedef struct painn_grad_norm painn_grad_norm;
+/* A table of n_tensors tensors (host array).  The tensors stay the caller's and
+ * must live as long as it does.  Synchronises the stream.  Errors: PAINN_E_ARG
+ * (null pointers, n < 0, reserved not 0, an `out` that overlaps another array
+ * of the table, or its own grad other than as a whole), PAINN_E_UNSUPPORTED
+ * (precision; 2^31 or more pieces of 8192 values), PAINN_E_OOM. */
+painn_status painn_grad_norm_create(painn_ctx* ctx, int32_t n_tensors, const painn_grad_tensor* tensors,
+                                    painn_grad_norm** out);
+/* result [2] (device FP32): the norm and the factor for max_norm (>= 0, may be
+ * infinite), of the gradients as they are now.  The blocks' sums are kept with
+ * the table: calls on one table are ordered by the caller.  After
+ * painn_destroy of its context a table refuses every call (PAINN_E_ARG) and can
+ * still be freed. */
+painn_status painn_grad_norm_compute(painn_grad_norm* table, double max_norm, float* result);
+/* The same, and writes every tensor's clipped gradients to its out (PAINN_E_ARG
+ * if one has none).  In place nothing is written where the factor is 1. */
+painn_status painn_grad_norm_clip(painn_grad_norm* table, double max_norm, float* result);
+painn_status painn_grad_norm_free(painn_grad_norm* table);
+
 /* AdamW over many tensors in one launch: FP32 parameters, FP32 or BF16
  * gradients, an optional BF16 copy of the parameters for the products, states
  * in FP32 or 8 bits.  With t the number of the step,
@@ -495,6 +619,9 @@ painn_status painn_adamw_create(painn_ctx* ctx, int32_t n_tensors, const painn_a
  * the lr and step number of its capture.  After painn_destroy of its context
  * an optimizer refuses every step (PAINN_E_ARG) and can still be freed. */
 painn_status painn_adamw_step(painn_adamw* opt, double lr);
+/* The same on gradients times *grad_scale (device FP32, read when the step
+ * runs: painn_grad_norm_compute's factor clips them; NULL: as they are). */
+painn_status painn_adamw_step_scaled(painn_adamw* opt, double lr, const float* grad_scale);
 /* Steps made so far (host). */
 painn_status painn_adamw_steps(const painn_adamw* opt, int64_t* steps);
 painn_status painn_adamw_free(painn_adamw* opt);

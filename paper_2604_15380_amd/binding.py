@@ -21,7 +21,10 @@ EXPORTS = [
     "painn_trainer_create", "painn_trainer_step", "painn_trainer_params", "painn_trainer_free",
     "painn_layer_norm", "painn_layer_norm_backward", "painn_linear", "painn_linear_backward",
     "painn_grouped_linear", "painn_grouped_linear_backward",
-    "painn_adamw_create", "painn_adamw_step", "painn_adamw_steps", "painn_adamw_free",
+    "painn_group_norm", "painn_group_norm_backward", "painn_group_norm_workspace",
+    "painn_gate", "painn_gate_backward", "painn_gate_workspace",
+    "painn_grad_norm_create", "painn_grad_norm_compute", "painn_grad_norm_clip", "painn_grad_norm_free",
+    "painn_adamw_create", "painn_adamw_step", "painn_adamw_step_scaled", "painn_adamw_steps", "painn_adamw_free",
     "painn_profile_enable",
     "painn_profile_read",
 ]
@@ -67,7 +70,18 @@ _SIGS = {
     "painn_grouped_linear": ([_P, _P, _I32, _P], ctypes.c_int),
     "painn_grouped_linear_backward": ([_P, _P, _I32, _P], ctypes.c_int),
     "painn_adamw_create": ([_P, _I32, _P, _P, ctypes.POINTER(_P)], ctypes.c_int),
+    "painn_group_norm": ([_P, _P], ctypes.c_int),
+    "painn_group_norm_backward": ([_P, _P, _P, _I64, _P, _I64, _P, _P], ctypes.c_int),
+    "painn_group_norm_workspace": ([ctypes.c_int, _I64, _I32, _I32, _I32, _I64, _I64, _I32], _I64),
+    "painn_gate": ([_P, _P], ctypes.c_int),
+    "painn_gate_backward": ([_P, _P, _P, ctypes.c_double, _P, _I64], ctypes.c_int),
+    "painn_gate_workspace": ([ctypes.c_int, _I64, _I32, _I32], _I64),
+    "painn_grad_norm_create": ([_P, _I32, _P, ctypes.POINTER(_P)], ctypes.c_int),
+    "painn_grad_norm_compute": ([_P, ctypes.c_double, _P], ctypes.c_int),
+    "painn_grad_norm_clip": ([_P, ctypes.c_double, _P], ctypes.c_int),
+    "painn_grad_norm_free": ([_P], ctypes.c_int),
     "painn_adamw_step": ([_P, ctypes.c_double], ctypes.c_int),
+    "painn_adamw_step_scaled": ([_P, ctypes.c_double, _P], ctypes.c_int),
     "painn_adamw_steps": ([_P, ctypes.POINTER(_I64)], ctypes.c_int),
     "painn_adamw_free": ([_P], ctypes.c_int),
     "painn_profile_enable": ([_P, ctypes.c_int], ctypes.c_int),
@@ -328,6 +342,81 @@ def painn_grouped_linear_backward(ctx: int, args, n_groups: int, offsets: int | 
     _check(load_library().painn_grouped_linear_backward(ctx, _struct_at(args), n_groups, offsets), ctx)
 
 
+class painn_group_norm_args(ctypes.Structure):
+    """include/painn.h painn_group_norm_args (host struct)."""
+    _fields_ = [("precision", _I32), ("activation", _I32), ("rows", _I64), ("cols", _I32), ("groups", _I32),
+                ("offsets", _P), ("sample_rows", _I64), ("n_samples", _I32), ("reserved", _I32), ("max_rows", _I64),
+                ("eps", ctypes.c_double), ("x", _P), ("ldx", _I64), ("gamma", _P), ("beta", _P), ("y", _P),
+                ("ldy", _I64), ("mean", _P), ("rstd", _P), ("workspace", _P), ("workspace_bytes", _I64)]
+
+
+class painn_gate_args(ctypes.Structure):
+    """include/painn.h painn_gate_args (host struct)."""
+    _fields_ = [("precision", _I32), ("heads", _I32), ("rows", _I64), ("k", _I32), ("normalize", _I32),
+                ("logits", _P), ("ldx", _I64), ("weights", _P), ("indices", _P), ("counts", _P), ("share", _P),
+                ("loss", _P), ("workspace", _P), ("workspace_bytes", _I64)]
+
+
+group_norm_args = struct.Struct("@iiqiiPqiiqdPqPPPqPPPq").pack
+gate_args = struct.Struct("@iiqiiPqPPPPPPq").pack
+assert struct.calcsize("@iiqiiPqiiqdPqPPPqPPPq") == ctypes.sizeof(painn_group_norm_args)
+assert struct.calcsize("@iiqiiPqPPPPPPq") == ctypes.sizeof(painn_gate_args)
+
+
+def painn_group_norm(ctx: int, args) -> None:
+    """args: a painn_group_norm_args or group_norm_args(...)."""
+    _check(load_library().painn_group_norm(ctx, _struct_at(args)), ctx)
+
+
+def painn_group_norm_backward(ctx: int, args, dy: int | None, lddy: int, dx: int | None, lddx: int,
+                              dgamma: int | None, dbeta: int | None) -> None:
+    _check(load_library().painn_group_norm_backward(ctx, _struct_at(args), dy, lddy, dx, lddx, dgamma, dbeta), ctx)
+
+
+def painn_group_norm_workspace(precision: int, rows: int, cols: int, groups: int, n_samples: int, sample_rows: int,
+                               max_rows: int, backward: bool) -> int:
+    return load_library().painn_group_norm_workspace(precision, rows, cols, groups, n_samples, sample_rows, max_rows,
+                                                     backward)
+
+
+def painn_gate(ctx: int, args) -> None:
+    """args: a painn_gate_args or gate_args(...)."""
+    _check(load_library().painn_gate(ctx, _struct_at(args)), ctx)
+
+
+def painn_gate_backward(ctx: int, args, dweights: int | None, balance: float, dlogits: int | None, ldd: int) -> None:
+    _check(load_library().painn_gate_backward(ctx, _struct_at(args), dweights, balance, dlogits, ldd), ctx)
+
+
+def painn_gate_workspace(precision: int, rows: int, heads: int, k: int) -> int:
+    return load_library().painn_gate_workspace(precision, rows, heads, k)
+
+
+class painn_grad_tensor(ctypes.Structure):
+    """include/painn.h painn_grad_tensor (host struct)."""
+    _fields_ = [("n", _I64), ("grad", _P), ("out", _P), ("precision", _I32), ("reserved", _I32)]
+
+
+def painn_grad_norm_create(ctx: int, tensors) -> int:
+    """tensors: dicts of painn_grad_tensor's fields (absent: null)."""
+    out = _P()
+    t = (painn_grad_tensor * max(1, len(tensors)))(*[painn_grad_tensor(**x) for x in tensors])
+    _check(load_library().painn_grad_norm_create(ctx, len(tensors), ctypes.addressof(t), ctypes.byref(out)), ctx)
+    return out.value
+
+
+def painn_grad_norm_compute(ctx: int, table: int, max_norm: float, result: int) -> None:
+    _check(load_library().painn_grad_norm_compute(table, max_norm, result), ctx)
+
+
+def painn_grad_norm_clip(ctx: int, table: int, max_norm: float, result: int) -> None:
+    _check(load_library().painn_grad_norm_clip(table, max_norm, result), ctx)
+
+
+def painn_grad_norm_free(table: int) -> None:
+    _check(load_library().painn_grad_norm_free(table))
+
+
 class painn_adamw_tensor(ctypes.Structure):
     """include/painn.h painn_adamw_tensor (host struct)."""
     _fields_ = [("n", _I64), ("param", _P), ("grad", _P), ("copy", _P), ("m", _P), ("v", _P), ("m_scale", _P),
@@ -366,6 +455,10 @@ def painn_adamw_create(ctx: int, tensors, cfg: dict) -> int:
 
 def painn_adamw_step(ctx: int, opt: int, lr: float) -> None:
     _check(load_library().painn_adamw_step(opt, lr), ctx)
+
+
+def painn_adamw_step_scaled(ctx: int, opt: int, lr: float, grad_scale: int | None) -> None:
+    _check(load_library().painn_adamw_step_scaled(opt, lr, grad_scale), ctx)
 
 
 def painn_adamw_steps(opt: int) -> int:

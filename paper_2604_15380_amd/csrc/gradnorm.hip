@@ -1,0 +1,270 @@
+// The global norm of the gradients of many tensors, and clipping.
+//
+// One pass over the gradients for the norm: each block walks over pieces of
+// 8,192 values of one tensor (a table made once says which) and adds squares in
+// FP64, so that no square leaves the range and the sum's order costs no digits;
+// the blocks' sums are added in their order.  Clipping is a second pass, or no
+// pass at all where the optimizer's step takes the factor.  Bound by memory.
+#include <math.h>
+
+#include <algorithm>
+#include <new>
+#include <vector>
+
+#include "ops.h"
+
+struct painn_grad_norm {
+  painn_ctx* ctx = nullptr;       // null: the context has been destroyed
+  painn_grad_norm *prev = nullptr, *next = nullptr;  // of the context's
+  long long pieces = 0;
+  bool outs = true;               // every tensor has a place for its clipped values
+  void* table = nullptr;          // GradTensor [n_tensors], Piece [pieces], double [GRID]
+  const void* piece_list = nullptr;
+  double* part = nullptr;
+};
+
+namespace {
+
+using namespace ops;
+
+constexpr int PIECE = 8192, GRID = 1024, TB = 256;
+
+struct GradTensor {
+  long long n;
+  const void* g;
+  void* out;
+  int bf16, unused;
+};
+struct Piece {
+  int tensor, index;              // values [8192 index, 8192 (index + 1)) of the tensor
+};
+
+__device__ __forceinline__ double block_sum(double s, double* lds) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
+  __syncthreads();
+  s = 0.0;
+  for (int w = 0; w < (int)blockDim.x / 64; ++w) s += lds[w];
+  return s;
+}
+
+template <class T>
+__device__ __forceinline__ void add_squares(const T* g, long long left, double* s) {
+  constexpr int V = 16 / sizeof(T), STEPS = PIECE / (TB * V);
+  float x[STEPS][V];
+#pragma unroll
+  for (int j = 0; j < STEPS; ++j) {
+    const int at = (j * TB + (int)threadIdx.x) * V;
+    load_n<V>(g + at, left - at, x[j]);
+  }
+#pragma unroll
+  for (int j = 0; j < STEPS; ++j)
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const double d = (double)x[j][i];
+      s[i & 1] = __builtin_fma(d, d, s[i & 1]);
+    }
+}
+
+__global__ void __launch_bounds__(TB) k_grad_squares(const GradTensor* __restrict__ tensors,
+                                                     const Piece* __restrict__ pieces, long long n,
+                                                     double* __restrict__ part) {
+  __shared__ double lds[TB / 64];
+  double s[2] = {0.0, 0.0};
+  for (long long k = blockIdx.x; k < n; k += gridDim.x) {
+    const Piece c = pieces[k];
+    const GradTensor t = tensors[c.tensor];
+    const long long at = (long long)c.index * PIECE;
+    if (t.bf16) add_squares((const b16*)t.g + at, t.n - at, s);
+    else add_squares((const float*)t.g + at, t.n - at, s);
+  }
+  const double sum = block_sum(s[0] + s[1], lds);
+  if (threadIdx.x == 0) part[blockIdx.x] = sum;
+}
+
+// result: the norm and the factor that takes it to max_norm at most.
+__global__ void __launch_bounds__(TB) k_grad_fold(const double* __restrict__ part, int n, double max_norm,
+                                                  float* __restrict__ result) {
+  __shared__ double lds[TB / 64];
+  double s = 0.0;
+  for (int k = threadIdx.x; k < n; k += TB) s += part[k];
+  const double norm = sqrt(block_sum(s, lds));
+  if (threadIdx.x == 0) {
+    result[0] = (float)norm;
+    result[1] = norm != norm ? (float)norm : norm > max_norm ? (float)(max_norm / norm) : 1.f;
+  }
+}
+
+template <class T>
+__device__ __forceinline__ void scale(const T* g, T* out, long long left, float f) {
+  constexpr int V = 16 / sizeof(T), STEPS = PIECE / (TB * V);
+  float x[STEPS][V];
+#pragma unroll
+  for (int j = 0; j < STEPS; ++j) {
+    const int at = (j * TB + (int)threadIdx.x) * V;
+    load_n<V>(g + at, left - at, x[j]);
+  }
+#pragma unroll
+  for (int j = 0; j < STEPS; ++j) {
+    const int at = (j * TB + (int)threadIdx.x) * V;
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[j][i] *= f;
+    store_n<V>(out + at, left - at, x[j]);
+  }
+}
+
+__global__ void __launch_bounds__(TB) k_grad_scale(const GradTensor* __restrict__ tensors,
+                                                   const Piece* __restrict__ pieces, long long n,
+                                                   const float* __restrict__ result) {
+  const float f = result[1];
+  for (long long k = blockIdx.x; k < n; k += gridDim.x) {
+    const Piece c = pieces[k];
+    const GradTensor t = tensors[c.tensor];
+    if (f == 1.f && t.out == t.g) continue;
+    const long long at = (long long)c.index * PIECE;
+    if (t.bf16) scale((const b16*)t.g + at, (b16*)t.out + at, t.n - at, f);
+    else scale((const float*)t.g + at, (float*)t.out + at, t.n - at, f);
+  }
+}
+
+painn_status norm_of(painn_grad_norm* h, double max_norm, float* result, bool clip) {
+  if (!h || !h->ctx) return PAINN_E_ARG;
+  painn_ctx* ctx = h->ctx;
+  ctx->err.clear();
+  if (!(max_norm >= 0.0)) return fail(ctx, PAINN_E_ARG, "max_norm must not be negative");
+  if (!result) return fail(ctx, PAINN_E_ARG, "null result");
+  if (clip && !h->outs) return fail(ctx, PAINN_E_ARG, "a tensor has no place for its clipped values");
+  (void)hipSetDevice(ctx->device);
+  (void)hipGetLastError();
+  const GradTensor* tt = (const GradTensor*)h->table;
+  const Piece* pp = (const Piece*)h->piece_list;
+  const int grid = (int)(h->pieces < GRID ? h->pieces : GRID);
+  prof_mark(ctx->prof, ctx->stream, KC_GRAD_NORM, true);
+  if (grid) k_grad_squares<<<grid, TB, 0, ctx->stream>>>(tt, pp, h->pieces, h->part);
+  k_grad_fold<<<1, TB, 0, ctx->stream>>>(h->part, grid, max_norm, result);
+  if (grid && clip) k_grad_scale<<<grid, TB, 0, ctx->stream>>>(tt, pp, h->pieces, result);
+  prof_mark(ctx->prof, ctx->stream, KC_GRAD_NORM, false);
+  return launched(ctx, "gradient norm launch");
+}
+
+}  // namespace
+
+extern "C" {
+
+painn_status painn_grad_norm_create(painn_ctx* ctx, int32_t n_tensors, const painn_grad_tensor* tensors,
+                                    painn_grad_norm** out) {
+  if (!ctx) return PAINN_E_ARG;
+  ctx->err.clear();
+  if (!out || n_tensors < 0 || (n_tensors > 0 && !tensors))
+    return fail(ctx, PAINN_E_ARG, "null argument or negative tensor count");
+  *out = nullptr;
+  long long pieces = 0;
+  bool outs = true;
+  for (int k = 0; k < n_tensors; ++k) {
+    const painn_grad_tensor& t = tensors[k];
+    const std::string what = "tensor " + std::to_string(k);
+    if (t.n < 0) return fail(ctx, PAINN_E_ARG, what + ": negative size");
+    if (t.precision != PAINN_FP32 && t.precision != PAINN_BF16)
+      return fail(ctx, PAINN_E_UNSUPPORTED, what + ": gradients are FP32 or BF16");
+    if (t.reserved) return fail(ctx, PAINN_E_ARG, what + ": reserved is not 0");
+    if (t.n > 0 && !t.grad) return fail(ctx, PAINN_E_ARG, what + ": null array");
+    constexpr long long most = 0x7fffffffLL;
+    if (t.n <= most * PIECE) pieces += (t.n + PIECE - 1) / PIECE;
+    if (t.n > most * PIECE || pieces > most) return fail(ctx, PAINN_E_UNSUPPORTED, "2^31 or more pieces of 8192 values");
+    outs = outs && (t.out || t.n == 0);
+  }
+  painn_grad_norm* h = nullptr;
+  try {
+    // what is written must be no other tensor's
+    struct Range {
+      uintptr_t a, b;
+      int tensor, written;
+    };
+    std::vector<Range> ranges;
+    for (int k = 0; k < n_tensors; ++k) {
+      const painn_grad_tensor& t = tensors[k];
+      const uintptr_t size = (uintptr_t)t.n * (t.precision == PAINN_BF16 ? 2 : 4);
+      if (!size) continue;
+      if (t.out != t.grad) ranges.push_back(Range{(uintptr_t)t.grad, (uintptr_t)t.grad + size, k, 0});
+      if (t.out) ranges.push_back(Range{(uintptr_t)t.out, (uintptr_t)t.out + size, k, 1});
+    }
+    std::sort(ranges.begin(), ranges.end(), [](const Range& x, const Range& y) { return x.a < y.a; });
+    // the farthest end so far of all ranges, and of the written ones
+    uintptr_t end = 0, end_written = 0;
+    for (const Range& r : ranges) {
+      if (r.a < (r.written ? end : end_written))
+        return fail(ctx, PAINN_E_ARG, "tensor " + std::to_string(r.tensor) + " overlaps one that clipping writes");
+      end = std::max(end, r.b);
+      if (r.written) end_written = std::max(end_written, r.b);
+    }
+    h = new (std::nothrow) painn_grad_norm();
+    if (!h) return fail(ctx, PAINN_E_OOM, "host allocation failed");
+    h->ctx = ctx;
+    h->next = ctx->grad_norms;
+    if (h->next) h->next->prev = h;
+    ctx->grad_norms = h;
+    h->pieces = pieces;
+    h->outs = outs;
+    const size_t head = align256((size_t)n_tensors * sizeof(GradTensor));
+    const size_t body = align256((size_t)pieces * sizeof(Piece)), bytes = head + body;
+    std::vector<unsigned char> host(bytes);
+    GradTensor* ht = (GradTensor*)host.data();
+    Piece* hp = (Piece*)(host.data() + head);
+    for (int k = 0; k < n_tensors; ++k) {
+      const painn_grad_tensor& t = tensors[k];
+      ht[k] = GradTensor{t.n, t.grad, t.out, t.precision == PAINN_BF16, 0};
+      for (long long i = 0; i * PIECE < t.n; ++i) *hp++ = Piece{k, (int)i};
+    }
+    (void)hipSetDevice(ctx->device);
+    hipError_t e = hipMalloc(&h->table, bytes + GRID * sizeof(double));
+    if (e == hipSuccess && bytes) e = hipMemcpyAsync(h->table, host.data(), bytes, hipMemcpyHostToDevice, ctx->stream);
+    if (e == hipSuccess) e = hipStreamSynchronize(ctx->stream);
+    if (e != hipSuccess) {
+      (void)hipGetLastError();
+      painn_grad_norm_free(h);
+      return fail(ctx, PAINN_E_OOM, std::string("gradient table: ") + hipGetErrorString(e));
+    }
+    h->piece_list = (const char*)h->table + head;
+    h->part = (double*)((char*)h->table + bytes);
+  } catch (...) {
+    if (h) painn_grad_norm_free(h);
+    return fail(ctx, PAINN_E_OOM, "host allocation failed");
+  }
+  *out = h;
+  return PAINN_OK;
+}
+
+painn_status painn_grad_norm_compute(painn_grad_norm* h, double max_norm, float* result) {
+  return norm_of(h, max_norm, result, false);
+}
+
+painn_status painn_grad_norm_clip(painn_grad_norm* h, double max_norm, float* result) {
+  return norm_of(h, max_norm, result, true);
+}
+
+painn_status painn_grad_norm_free(painn_grad_norm* h) {
+  if (!h) return PAINN_OK;
+  if (h->ctx) {
+    (void)hipSetDevice(h->ctx->device);
+    (void)hipStreamSynchronize(h->ctx->stream);
+    if (h->prev) h->prev->next = h->next;
+    else h->ctx->grad_norms = h->next;
+    if (h->next) h->next->prev = h->prev;
+  }
+  if (h->table) (void)hipFree(h->table);
+  delete h;
+  return PAINN_OK;
+}
+
+}  // extern "C"
+
+void grad_norm_detach(painn_ctx* ctx) {
+  for (painn_grad_norm *h = ctx->grad_norms, *next; h; h = next) {
+    next = h->next;
+    h->ctx = nullptr;
+    h->prev = h->next = nullptr;
+  }
+  ctx->grad_norms = nullptr;
+}

@@ -187,6 +187,8 @@ struct painn_ctx {
   Workspace ows;
   // its optimizers (optim.hip): one may outlive the context
   painn_adamw* optimizers = nullptr;
+  // and its gradient norms (gradnorm.hip)
+  painn_grad_norm* grad_norms = nullptr;
 };
 
 struct painn_model {

@@ -6,10 +6,11 @@
 // on its way meanwhile.  Rows too long for that are read again for each.  The
 // lanes walk over the rows, so that gamma and beta are loaded once and the
 // reverse pass's column sums (dgamma, dbeta) stay in registers until the end;
-// each block then writes one partial row and k_norm_fold adds the blocks'
+// each block then writes one partial row and k_fold adds the blocks'
 // partials in their order.  Bound by memory.
 #include <type_traits>
 
+#include "fold.h"
 #include "ops.h"
 
 namespace {
@@ -269,32 +270,6 @@ __global__ void __launch_bounds__(TB) k_norm_cols(long long rows, int cols, cons
   part[((size_t)blockIdx.y * 2 + 1) * cols + c] = db;
 }
 
-// dgamma (blockIdx.y = 0) or dbeta (1): 32 columns per block at a time, the
-// partial rows in 32 slices.
-template <class T>
-__global__ void __launch_bounds__(1024) k_norm_fold(int n, int cols, const float* __restrict__ part,
-                                                    T* __restrict__ dgamma, T* __restrict__ dbeta) {
-  __shared__ float s[32][33];
-  const int q = threadIdx.x >> 5, l = threadIdx.x & 31;
-  for (int c0 = blockIdx.x * 32; c0 < cols; c0 += gridDim.x * 32) {
-    const int c = c0 + l;
-    float a = 0.f;
-    if (c < cols) {
-#pragma unroll 8
-      for (int k = q; k < n; k += 32) a += part[((size_t)k * 2 + blockIdx.y) * cols + c];
-    }
-    s[q][l] = a;
-    __syncthreads();
-    if (q == 0 && c < cols) {
-      a = 0.f;
-#pragma unroll
-      for (int k = 0; k < 32; ++k) a += s[k][l];
-      store<1>((blockIdx.y ? dbeta : dgamma) + c, &a);
-    }
-    __syncthreads();
-  }
-}
-
 struct NormArgs {
   painn_ctx* ctx;
   long long rows;
@@ -309,7 +284,6 @@ struct NormArgs {
 
 constexpr int NORM_GRID = 2048;     // blocks of a launch: 8 per CU
 constexpr int NORM_GRID_BWD = 1024; // and of the reverse pass, whose partial rows are folded
-constexpr int NORM_FOLD = 65536;    // and of that, along the columns
 constexpr int NORM_COLS = 1 << 30;  // a row's columns at most: their count steps by up to 2^21 in an int
 
 inline int grid_for(long long rows, int rpb, int most) {
@@ -394,8 +368,7 @@ painn_status run_norm_bwd(const NormArgs& a) {
                                                        (const T*)a.gamma, a.mu, a.rs, (T*)a.dx, a.lddx);
   }
   if (a.dgamma)
-    k_norm_fold<T><<<dim3(grid_for(c, 32, NORM_FOLD), 2), 1024, 0, ctx->stream>>>(slices, c, part, (T*)a.dgamma,
-                                                                                (T*)a.dbeta);
+    fold_columns<T>(ctx->stream, slices, c, part, (T*)a.dgamma, (T*)a.dbeta);
   prof_mark(ctx->prof, ctx->stream, KC_NORM_BWD, false);
   return launched(ctx, "layer norm reverse launch");
 }

@@ -1,12 +1,15 @@
-// Shared by the head-tuning operators (norm.hip, dense.hip, optim.hip): typed
-// loads and stores, wave sums, activations, their timing classes and their
-// workspace.
+// Shared by the head-tuning operators (norm.hip, groupnorm.hip, dense.hip,
+// gate.hip, optim.hip, gradnorm.hip): typed loads and stores, wave sums,
+// activations, their timing classes and their workspace.
 #pragma once
 
 #include "internal.h"
 
 // timing classes, after those of the model's kernels
-enum OpsKernelClass { KC_NORM = KC_COUNT, KC_NORM_BWD, KC_LINEAR, KC_LINEAR_BWD, KC_ADAMW, KC_ALL };
+enum OpsKernelClass {
+  KC_NORM = KC_COUNT, KC_NORM_BWD, KC_LINEAR, KC_LINEAR_BWD, KC_ADAMW, KC_GROUP_NORM, KC_GROUP_NORM_BWD, KC_GATE,
+  KC_GATE_BWD, KC_GRAD_NORM, KC_ALL
+};
 
 // Room for `need` bytes in the context's workspace ows.  PAINN_E_OOM
 // where it cannot be had, or only by allocating while the stream is captured.
@@ -14,6 +17,8 @@ painn_status ops_workspace(painn_ctx* ctx, size_t need);
 
 // The context ends: its optimizers refuse every further step.
 void adamw_detach(painn_ctx* ctx);
+// ... and so do its gradient norms.
+void grad_norm_detach(painn_ctx* ctx);
 
 namespace ops {
 

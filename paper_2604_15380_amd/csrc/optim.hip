@@ -130,7 +130,8 @@ __device__ __forceinline__ void store_codes(uint8_t* p, long long n, uint32_t w)
 
 template <class G, bool Q8>
 __global__ void __launch_bounds__(256) k_adamw(const AdamTensor* __restrict__ tensors,
-                                               const Chunk* __restrict__ chunks, AdamScalars s) {
+                                               const Chunk* __restrict__ chunks, AdamScalars s,
+                                               const float* __restrict__ grad_scale) {
   const Chunk c = chunks[blockIdx.x];
   const AdamTensor t = tensors[c.tensor];
   const int lane = threadIdx.x & 63;
@@ -138,6 +139,11 @@ __global__ void __launch_bounds__(256) k_adamw(const AdamTensor* __restrict__ te
   float p[4], g[4], m[4], v[4], root[4];
   load_n<4>(t.p + i, left, p);
   load_n<4>((const G*)t.g + i, left, g);
+  if (grad_scale) {
+    const float f = *grad_scale;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) g[e] = e < left ? g[e] * f : 0.f;
+  }
   if constexpr (Q8) {
     const uint32_t mc = load_codes((const uint8_t*)t.m + i, left), vc = load_codes((const uint8_t*)t.v + i, left);
     decode(mc, b < t.n ? t.ms[b / QBLOCK] : 0.f, m);
@@ -242,7 +248,9 @@ painn_status painn_adamw_create(painn_ctx* ctx, int32_t n_tensors, const painn_a
   return PAINN_OK;
 }
 
-painn_status painn_adamw_step(painn_adamw* opt, double lr) {
+painn_status painn_adamw_step(painn_adamw* opt, double lr) { return painn_adamw_step_scaled(opt, lr, nullptr); }
+
+painn_status painn_adamw_step_scaled(painn_adamw* opt, double lr, const float* grad_scale) {
   if (!opt || !opt->ctx) return PAINN_E_ARG;
   painn_ctx* ctx = opt->ctx;
   ctx->err.clear();
@@ -263,10 +271,10 @@ painn_status painn_adamw_step(painn_adamw* opt, double lr) {
     const dim3 grid((unsigned)opt->chunks);
     const bool q8 = c.state_bits == 8, g16 = c.grad_precision == PAINN_BF16;
     prof_mark(ctx->prof, ctx->stream, KC_ADAMW, true);
-    if (q8 && g16) k_adamw<b16, true><<<grid, 256, 0, ctx->stream>>>(tt, cc, s);
-    else if (q8) k_adamw<float, true><<<grid, 256, 0, ctx->stream>>>(tt, cc, s);
-    else if (g16) k_adamw<b16, false><<<grid, 256, 0, ctx->stream>>>(tt, cc, s);
-    else k_adamw<float, false><<<grid, 256, 0, ctx->stream>>>(tt, cc, s);
+    if (q8 && g16) k_adamw<b16, true><<<grid, 256, 0, ctx->stream>>>(tt, cc, s, grad_scale);
+    else if (q8) k_adamw<float, true><<<grid, 256, 0, ctx->stream>>>(tt, cc, s, grad_scale);
+    else if (g16) k_adamw<b16, false><<<grid, 256, 0, ctx->stream>>>(tt, cc, s, grad_scale);
+    else k_adamw<float, false><<<grid, 256, 0, ctx->stream>>>(tt, cc, s, grad_scale);
     prof_mark(ctx->prof, ctx->stream, KC_ADAMW, false);
     const painn_status st = launched(ctx, "optimizer step launch");
     if (st != PAINN_OK) return st;

@@ -460,7 +460,8 @@ static const char* kc_name(int kc) {
                                         "embed", "phi", "edge_prep", "message", "update", "heads",
                                         "energy", "export", "transpose", "bwd_heads", "bwd_update",
                                         "bwd_message", "bwd_phi", "force", "train_real", "train_tangent",
-                                        "train_adamw", "norm", "bwd_norm", "linear", "bwd_linear", "adamw"};
+                                        "train_adamw", "norm", "bwd_norm", "linear", "bwd_linear", "adamw",
+                                        "group_norm", "bwd_group_norm", "gate", "bwd_gate", "grad_norm"};
   return names[kc];
 }
 
@@ -564,6 +565,7 @@ painn_status painn_destroy(painn_ctx* ctx) {
   if (ctx->h_status) (void)hipHostFree(ctx->h_status);
   prof_free(ctx->prof);
   adamw_detach(ctx);
+  grad_norm_detach(ctx);
   delete ctx;
   return PAINN_OK;
 }

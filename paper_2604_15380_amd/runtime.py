@@ -4,6 +4,7 @@ from __future__ import annotations
 
 import ctypes
 import sys
+import typing
 
 import numpy as np
 
@@ -138,14 +139,21 @@ class AdamW:
         self.handle = B.painn_adamw_create(rt.ctx, B.adamw_tensors(fields), cfg)
         rt._leave(cur, ())
 
-    def step(self, lr=None):
+    def step(self, lr=None, grad_scale=None):
         """One step on the gradients as they are now, at `lr` or the one given
-        at the start."""
+        at the start.  grad_scale: one float32 on the GPU that the gradients
+        are multiplied by (GradNorm.compute's factor clips them)."""
+        scale = 0
+        if grad_scale is not None:
+            import torch
+            if grad_scale.dtype is not torch.float32 or grad_scale.numel() != 1 or grad_scale.device != self.rt.device:
+                raise ValueError(f"grad_scale must be one float32 value on {self.rt.device}")
+            scale = grad_scale.data_ptr()
         cur = self.rt._enter()
-        B.painn_adamw_step(self.rt.ctx, self.handle, self.lr if lr is None else lr)
+        B.painn_adamw_step_scaled(self.rt.ctx, self.handle, self.lr if lr is None else lr, scale)
         if cur is not None:
-            self.rt._leave(cur, [t for a in (self.params, self.grads, self.copies, self.m, self.v,
-                                             self.m_scale or (), self.v_scale or ()) for t in a if t is not None])
+            self.rt._leave(cur, [t for a in (self.params, self.grads, self.copies, self.m, self.v, self.m_scale or (),
+                                             self.v_scale or (), (grad_scale,)) for t in a if t is not None])
 
     @property
     def steps(self):
@@ -166,6 +174,75 @@ class AdamW:
     def __del__(self):
         if getattr(self, "handle", 0) and sys is not None and not sys.is_finalizing():
             self.free()
+
+
+class GradNorm:
+    """The global norm of many tensors' gradients and clipping by it
+    (painn_grad_norm_*).
+
+    The tensors are read where they were when this was made.  `outs`: where
+    clip writes, by default the gradients themselves."""
+
+    def __init__(self, rt, grads, outs=None):
+        grads = list(grads)
+        outs = list(outs) if outs is not None else grads
+        if len(outs) != len(grads):
+            raise ValueError("grads and outs differ in length")
+        dev, table = rt.device, []
+        for k, (g, o) in enumerate(zip(grads, outs)):
+            for name, a in (("grad", g), ("out", o)):
+                if _precisions().get(a.dtype) is None or a.dtype is not g.dtype or a.numel() != g.numel() or \
+                        not a.is_contiguous() or a.device != dev:
+                    raise ValueError(f"tensor {k}: {name} must be contiguous float32 or bfloat16 of {g.numel()} values, "
+                                     f"as its grad, on {dev}")
+            table.append(dict(n=g.numel(), grad=g.data_ptr(), out=o.data_ptr(), precision=_precisions()[g.dtype]))
+        self.rt, self.grads, self.outs, self.handle = rt, grads, outs, 0
+        cur = rt._enter()
+        self.handle = B.painn_grad_norm_create(rt.ctx, table)
+        rt._leave(cur, ())
+
+    def _run(self, fn, max_norm):
+        import torch
+        result = torch.empty(2, dtype=torch.float32, device=self.rt.device)
+        cur = self.rt._enter()
+        fn(self.rt.ctx, self.handle, max_norm, result.data_ptr())
+        if cur is not None:
+            self.rt._leave(cur, self.grads + self.outs + [result])
+        return result.unbind()
+
+    def compute(self, max_norm=float("inf")):
+        """(norm, factor) of the gradients as they are now, each one float32 on
+        the GPU; factor takes them to max_norm at most (AdamW.step's
+        grad_scale)."""
+        return self._run(B.painn_grad_norm_compute, max_norm)
+
+    def clip(self, max_norm):
+        """Multiply every gradient by the factor (or write the products to
+        `outs`); returns the norm before."""
+        return self._run(B.painn_grad_norm_clip, max_norm)[0]
+
+    def free(self):
+        if self.handle:
+            B.painn_grad_norm_free(self.handle)
+        self.handle = 0
+
+    def __del__(self):
+        if getattr(self, "handle", 0) and sys is not None and not sys.is_finalizing():
+            self.free()
+
+
+class Gate(typing.NamedTuple):
+    """What Runtime.gate gives: weights and indices [rows, k] (float32, int32,
+    -1 for no head), counts and share [heads] (int32, float32), the balance
+    loss (float32), and `totals` [heads + 1], the counts with the number of
+    rows that have a head, for the reverse pass."""
+    weights: object
+    indices: object
+    counts: object
+    share: object
+    loss: object
+    totals: object
+    normalize: bool
 
 
 _NAMES = {}
@@ -392,6 +469,138 @@ class Runtime:
             self._leave(cur, (dy, x, weight, mean, rstd, dx, dweight, dbias))
         return dx, dweight, dbias
 
+    def _samples(self, x, weight, bias, groups, offsets, sample_rows, activation):
+        """What both passes of group norm check: (precision, activation, rows,
+        cols, x's pointer and stride, weight, bias, offsets, samples, their rows)"""
+        import torch
+        prec, t = self._precision(x), x.dtype
+        if x.dim() != 2:
+            raise ValueError("x must be [rows, cols]")
+        n, c = x.shape
+        if not 0 < groups <= c or c % groups:
+            raise ValueError(f"{groups} groups do not divide {c} columns")
+        px, ldx = self._rows(x, "x", t, n, c)
+        pw, pb = self._whole(weight, "weight", t, (c,)), self._whole(bias, "bias", t, (c,))
+        if (offsets is None) == (sample_rows is None):
+            raise ValueError("samples are given by offsets or by sample_rows")
+        if offsets is not None:
+            if offsets.dim() != 1 or not len(offsets):
+                raise ValueError("offsets must be [samples + 1]")
+            samples, sample_rows = len(offsets) - 1, 0
+            po = self._whole(offsets, "offsets", torch.int32, (samples + 1,))
+        else:
+            if sample_rows < 1 or n % sample_rows:
+                raise ValueError(f"{n} rows are no multiple of sample_rows {sample_rows}")
+            samples, po = n // sample_rows, 0
+        return prec, self._activation(activation), n, c, px, ldx, pw, pb, po, samples, sample_rows
+
+    def group_norm(self, x, weight, bias, groups, offsets=None, sample_rows=None, activation="none", eps=1e-5,
+                   max_rows=None, out=None):
+        """(y, mean, rstd): group norm of x [rows, cols] with an activation.
+        Samples are the rows offsets[s] .. offsets[s+1] (int32 on the GPU) or
+        every sample_rows rows; a sample's rows and a group's columns share one
+        mean and rstd ([samples, groups], FP32).  max_rows, the longest sample
+        where the program knows it, saves a launch.  Rows of no sample are left
+        as they are in `out` (undefined in a new one); `out` may be x."""
+        import torch
+        prec, act, n, c, px, ldx, pw, pb, po, samples, each = self._samples(x, weight, bias, groups, offsets, sample_rows,
+                                                                           activation)
+        if out is None:
+            out = x.new_empty((n, c))
+        py, ldy = self._rows(out, "out", x.dtype, n, c)
+        stats = x.new_empty((2, samples, groups), dtype=torch.float32)
+        mean, rstd = stats.unbind()
+        longest = max_rows or 0
+        need = B.painn_group_norm_workspace(prec, n, c, groups, samples, each, longest, False)
+        ws = x.new_empty(need, dtype=torch.uint8) if need else None
+        cur = self._enter()
+        B.painn_group_norm(self.ctx, B.group_norm_args(
+            prec, act, n, c, groups, po, each, samples, 0, longest, eps, px, ldx, pw, pb, py, ldy, mean.data_ptr(),
+            rstd.data_ptr(), ws.data_ptr() if need else 0, need))
+        if cur is not None:
+            self._leave(cur, (x, weight, bias, offsets, out, stats, ws))
+        return out, mean, rstd
+
+    def group_norm_backward(self, dy, x, weight, bias, mean, rstd, groups, offsets=None, sample_rows=None,
+                            activation="none", max_rows=None, dx=None, dweight=None, dbias=None, need_dx=True):
+        """(dx, dweight, dbias) from dy and the forward's x, mean and rstd; the
+        activation's inputs are formed again.  dx is None without need_dx and
+        may be given as dy; its rows of no sample are left as they are."""
+        import torch
+        prec, act, n, c, px, ldx, pw, pb, po, samples, each = self._samples(x, weight, bias, groups, offsets, sample_rows,
+                                                                           activation)
+        pm, pr = (self._whole(a, k, torch.float32, (samples, groups)) for a, k in ((mean, "mean"), (rstd, "rstd")))
+        pd, ldd = self._rows(dy, "dy", x.dtype, n, c)
+        if not need_dx:
+            dx = None
+        elif dx is None:
+            dx = x.new_empty((n, c))
+        dweight = torch.empty_like(weight) if dweight is None else dweight
+        dbias = torch.empty_like(weight) if dbias is None else dbias
+        po_, ldo = self._rows(dx, "dx", x.dtype, n, c)
+        pg, pbb = self._whole(dweight, "dweight", x.dtype, (c,)), self._whole(dbias, "dbias", x.dtype, (c,))
+        longest = max_rows or 0
+        need = B.painn_group_norm_workspace(prec, n, c, groups, samples, each, longest, True)
+        ws = x.new_empty(need, dtype=torch.uint8) if need else None
+        cur = self._enter()
+        B.painn_group_norm_backward(self.ctx, B.group_norm_args(
+            prec, act, n, c, groups, po, each, samples, 0, longest, 0.0, px, ldx, pw, pb, 0, 0, pm, pr,
+            ws.data_ptr() if need else 0, need), pd, ldd, po_, ldo, pg, pbb)
+        if cur is not None:
+            self._leave(cur, (dy, x, weight, bias, mean, rstd, offsets, dx, dweight, dbias, ws))
+        return dx, dweight, dbias
+
+    def gate(self, logits, k, normalize=False) -> Gate:
+        """The k heads of every row of logits [rows, heads] with the largest
+        softmax weights, and what a balanced gate needs: counts, mean
+        probabilities and the balance loss, heads sum_h (counts[h] / sum
+        counts) share[h].  A logit of -inf is a head that the row cannot take.
+        normalize: a row's weights add up to 1."""
+        import torch
+        prec = self._precision(logits)
+        if logits.dim() != 2:
+            raise ValueError("logits must be [rows, heads]")
+        n, h = logits.shape
+        if not 0 < k <= h:
+            raise ValueError(f"k must be within 1 and {h} heads, not {k}")
+        px, ldx = self._rows(logits, "logits", logits.dtype, n, h)
+        new = lambda *s, dtype=torch.float32: logits.new_empty(s, dtype=dtype)  # noqa: E731
+        weights, indices, sums, totals = new(n, k), new(n, k, dtype=torch.int32), new(h + 1), new(h + 1, dtype=torch.int32)
+        share, loss = sums[:h], sums[h]
+        need = B.painn_gate_workspace(prec, n, h, k)
+        ws = new(need, dtype=torch.uint8) if need else None
+        at = sums.data_ptr()
+        cur = self._enter()
+        B.painn_gate(self.ctx, B.gate_args(prec, h, n, k, bool(normalize), px, ldx, weights.data_ptr(), indices.data_ptr(),
+                                           totals.data_ptr(), at, at + 4 * h, ws.data_ptr() if need else 0, need))
+        if cur is not None:
+            self._leave(cur, (logits, weights, indices, sums, totals, ws))
+        return Gate(weights, indices, totals[:h], share, loss, totals, bool(normalize))
+
+    def gate_backward(self, dweights, logits, gate, balance=0.0, dlogits=None):
+        """dlogits of (dweights weights) + balance loss, `gate` the forward's
+        result; dweights [rows, k] float32 or None (zero).  The counts are
+        constants of the loss.  Masked logits get 0.  dlogits may be the logits."""
+        import torch
+        prec = self._precision(logits)
+        if logits.dim() != 2:
+            raise ValueError("logits must be [rows, heads]")
+        n, h = logits.shape
+        k = gate.indices.shape[-1]
+        px, ldx = self._rows(logits, "logits", logits.dtype, n, h)
+        pi = self._whole(gate.indices, "indices", torch.int32, (n, k))
+        pt = self._whole(gate.totals, "totals", torch.int32, (h + 1,))
+        pd = self._whole(dweights, "dweights", torch.float32, (n, k))
+        if dlogits is None:
+            dlogits = logits.new_empty((n, h))
+        po, ldo = self._rows(dlogits, "dlogits", logits.dtype, n, h)
+        cur = self._enter()
+        B.painn_gate_backward(self.ctx, B.gate_args(prec, h, n, k, gate.normalize, px, ldx, 0, pi, pt, 0, 0, 0, 0), pd,
+                              balance, po, ldo)
+        if cur is not None:
+            self._leave(cur, (dweights, logits, gate.indices, gate.totals, dlogits))
+        return dlogits
+
     def _activation(self, name):
         try:
             return B.ACTIVATIONS[name]
@@ -521,6 +730,11 @@ class Runtime:
             raise ValueError("offsets is missing")
         return self._dense_backward(dy, x, weight, offsets, activation, preact, x_activation, x_preact, need_dx, dx,
                                     dweight, dbias, dz_remainders)
+
+    def grad_norm(self, grads, outs=None) -> GradNorm:
+        """The global norm of these gradients, and clipping (GradNorm's
+        arguments)."""
+        return GradNorm(self, grads, outs)
 
     def adamw(self, params, grads, **how) -> AdamW:
         """An optimizer of these tensors (AdamW's arguments)."""
