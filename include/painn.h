@@ -406,7 +406,7 @@ int64_t painn_group_norm_workspace(painn_precision precision, int64_t rows, int3
  * groups that do not divide cols, rows that are not n_samples sample_rows
  * without offsets, a stride below cols or another one in place, an unknown
  * activation, eps as in painn_layer_norm, reserved not 0, a workspace that is
- * too small), PAINN_E_UNSUPPORTED (FP64; more than 4096 columns in a group,
+ * too small), PAINN_E_UNSUPPORTED (FP64; more than 2048 columns in a group,
  * 2^24 columns or 2^31 - 1 rows; more blocks than a launch holds). */
 painn_status painn_group_norm(painn_ctx* ctx, const painn_group_norm_args* args);
 /* Its reverse pass, from dy = dL/dy and the forward's x, mean and rstd (y is

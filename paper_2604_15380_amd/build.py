@@ -18,7 +18,7 @@ CSRC = os.path.join(PKG, "csrc")
 OUT = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libpainn.so")
 SOURCES = ["runtime.cpp", "weightfile.cpp", "noalloc.hip", "neighbors.hip", "forward.hip", "branch.hip", "backward.hip",
-           "train.hip", "norm.hip", "groupnorm.hip", "dense.hip", "gate.hip", "optim.hip", "gradnorm.hip"]
+           "train.hip", "norm.hip", "groupnorm.hip", "groupnorm_bwd.hip", "dense.hip", "gate.hip", "optim.hip", "gradnorm.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -9,8 +9,6 @@ import torch
 import ops_reference as ref
 from ops_reference import E16, E32
 
-E64 = 2.0 ** -53
-
 
 def sample_spans(offsets, rows):
     return ref.spans(offsets, rows)
@@ -44,24 +42,37 @@ def per_row(stat, spans, rows, cg):
     return out
 
 
-def group_norm_bounds(x, g, b, mean, rstd, xh, z, spans, eps, kind, dtype):
+def group_norm_bounds(x, g, b, mean, rstd, xh, z, spans, eps, kind, dtype, terms=81, ratio=8):
     """Bounds of y, mean and rstd.
 
-    The sums are FP64: n of them leave n 2^-53 of the sum of squares, which is
-    (mean^2 + var) / (var + eps) times that of the variance.  The mean is
-    rounded once, rstd three times after the variance's own rounding (a square
-    root and a quotient of 1 and 2.5 steps, 8 E32 in all).  z passes the mean's
-    error, the difference's, the product's and the sum's rounding, 12 of them;
-    the activations, slope at most 1.13, are evaluated to 4 E32 |z|."""
+    Short samples: d = x - K and d^2 are summed in FP32, K the mean of at least
+    1 / ratio of the sample's rows (8: 64 rows where 8 are held; others hold a
+    quarter).  A sum passes at most `terms` additions: 3 in a vector, 64 rows
+    of a thread, 6 between lanes and 8 between waves.  n_held (K - mean)^2 <= n
+    var, and K's own sum is off by terms E32 max |x|, so that
+        |K - mean| <= k = sqrt(ratio var) + terms E32 max |x|,
+        mean |d| <= D = sqrt(var) + k,  mean d^2 = var + (K - mean)^2.
+    The mean is off by (terms + 3) E32 D and its rounding, the variance by
+    (terms + 6) E32 (var + k^2) and 2 k (terms + 3) E32 D, rstd by half of that
+    relative to var + eps and a square root's and a quotient's rounding (8 E32
+    in all).  Long samples are summed in FP64, which leaves less.  z passes the
+    mean's error, the difference's, the products' and the sum's rounding, 12 of
+    them; the activations, slope at most 1.13, are evaluated to 4 E32 |z|."""
     n, c = x.shape
     cg = c // mean.shape[1]
-    count = torch.tensor([max(1, (hi - lo) * cg) for lo, hi in spans], dtype=torch.float64)[:, None]
-    safe = rstd.clamp_min(1e-300)
-    noise = count * E64 * (mean ** 2 * safe ** 2 + 1)
-    bm = E32 * mean.abs() + count * E64 * (mean.abs() + 1 / safe) * (rstd > 0)
+    top, var, some = torch.zeros_like(mean), torch.zeros_like(mean), torch.zeros_like(mean)
+    for s, (lo, hi) in enumerate(spans):
+        if hi > lo:
+            v = x[lo:hi].view(hi - lo, -1, cg)
+            top[s], some[s] = v.abs().amax((0, 2)), 1
+            var[s] = ((v - v.mean((0, 2))[None, :, None]) ** 2).mean((0, 2))
+    k = (ratio * var).sqrt() + terms * E32 * top
+    d = var.sqrt() + k
+    bm = (E32 * mean.abs() + (terms + 3) * E32 * d) * some
+    noise = ((terms + 6) * E32 * (var + k ** 2) + 2 * k * (terms + 3) * E32 * d) * rstd ** 2 / 2
     br = rstd * (8 * E32 + noise)
-    mu, rs, er = (per_row(a, spans, n, cg) for a in (mean, rstd, noise))
-    bz = E32 * (rs * g.abs() * (mu.abs() + 12 * (x - mu).abs()) + 2 * b.abs() + z.abs()) + (xh * g).abs() * er
+    rs, er, em, mu = (per_row(a, spans, n, cg) for a in (rstd, noise, bm, mean))
+    bz = rs * g.abs() * (em + 12 * E32 * (x - mu).abs()) + E32 * (2 * b.abs() + z.abs()) + (xh * g).abs() * er
     by = 1.13 * bz + (4 * E32 * z.abs() if kind not in ("none", "relu") else 0)
     if dtype == torch.bfloat16:
         by = by + E16 * (ref.act(z, kind).abs() + by)
