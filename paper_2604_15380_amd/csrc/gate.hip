@@ -22,7 +22,8 @@ using namespace ops;
 
 constexpr int KREG = 8;             // heads chosen one after the other
 constexpr int HEADS = 1024;         // heads at most
-constexpr int GATE_GRID = 256;      // blocks of the forward, whose sums are folded
+constexpr int GATE_BWD = 2048;      // blocks of the reverse pass at most: 8 per CU
+constexpr int GATE_GRID = 512;      // blocks of the forward, whose sums are folded
 
 struct GateArgs {
   long long rows;
@@ -54,43 +55,52 @@ __device__ __forceinline__ float exp_of(float d) {
 }
 
 // Keys in the values' order; NaN above infinity, -0 as 0; 0 is below every key.
+// BF16's last 16 bits are 0, which leaves room for the head: 0xffff - head, so
+// that the lowest of equals has the largest key.
 __device__ __forceinline__ uint32_t ordered(float x) {
   const uint32_t u = __float_as_uint(x + 0.f);
   if ((u & 0x7fffffffu) > 0x7f800000u) return 0xffffffffu;
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
-__device__ __forceinline__ float value_of(uint32_t o) {
-  return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o);
+__device__ __forceinline__ float value_of(uint32_t o, bool bf16) {
+  return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : bf16 ? ~o & 0xffff0000u : ~o);
 }
-template <class T>
-struct Key;
-template <>
-struct Key<float> {
-  typedef unsigned long long type;
-  static __device__ __forceinline__ type make(float x, int e) {
-    return ((type)ordered(x) << 32) | (uint32_t)(0xffffffffu - (uint32_t)e);
-  }
-  static __device__ __forceinline__ float value(type k) { return value_of((uint32_t)(k >> 32)); }
-  static __device__ __forceinline__ int head(type k) { return (int)(0xffffffffu - (uint32_t)k); }
-};
-template <>
-struct Key<b16> {                   // BF16 has 16 bits, which leaves 16 for the head
-  typedef uint32_t type;
-  static __device__ __forceinline__ type make(float x, int e) {
-    return (ordered(x) & 0xffff0000u) | (0xffffu - (uint32_t)e);
-  }
-  static __device__ __forceinline__ float value(type k) {
-    const uint32_t o = k & 0xffff0000u;
-    return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o & 0xffff0000u);
-  }
-  static __device__ __forceinline__ int head(type k) { return (int)(0xffffu - (k & 0xffffu)); }
-};
-
+// x of a lane that has another part of the row's reduction: within 16 lanes the
+// exchange is part of the instruction that uses it.
+template <int O>
+__device__ __forceinline__ int lane_of(int x) {
+  if constexpr (O == 1) return __builtin_amdgcn_update_dpp(x, x, 0xb1, 0xf, 0xf, false);        // quad_perm 1, 0, 3, 2
+  else if constexpr (O == 2) return __builtin_amdgcn_update_dpp(x, x, 0x4e, 0xf, 0xf, false);   // quad_perm 2, 3, 0, 1
+  else if constexpr (O == 4) return __builtin_amdgcn_update_dpp(x, x, 0x141, 0xf, 0xf, false);  // 8 lanes mirrored
+  else if constexpr (O == 8) return __builtin_amdgcn_update_dpp(x, x, 0x140, 0xf, 0xf, false);  // 16 lanes mirrored
+  else if constexpr (O == 16) return __builtin_amdgcn_ds_swizzle(x, 0x401f);                    // xor 16
+  else return __shfl_xor(x, 32);
+}
+// The reduction of x over the row's LPR lanes, in all of them.
+template <int LPR, int O = 1, class F>
+__device__ __forceinline__ int lanes(int x, F&& f) {
+  if constexpr (O < LPR) return lanes<LPR, 2 * O>(f(x, lane_of<O>(x)), f);
+  else return x;
+}
 template <int LPR>
 __device__ __forceinline__ float lanes_sum(float x) {
-#pragma unroll
-  for (int o = LPR / 2; o; o >>= 1) x += __shfl_xor(x, o);
-  return x;
+  return __int_as_float(lanes<LPR>(__float_as_int(x), [](int p, int q) {
+    return __float_as_int(__int_as_float(p) + __int_as_float(q));
+  }));
+}
+template <int LPR>
+__device__ __forceinline__ int lanes_add(int x) {
+  return lanes<LPR>(x, [](int p, int q) { return p + q; });
+}
+template <int LPR>
+__device__ __forceinline__ float lanes_max(float x) {
+  return __int_as_float(lanes<LPR>(__float_as_int(x), [](int p, int q) {
+    return __float_as_int(fmaxf(__int_as_float(p), __int_as_float(q)));
+  }));
+}
+template <int LPR>
+__device__ __forceinline__ uint32_t lanes_max(uint32_t x) {
+  return (uint32_t)lanes<LPR>((int)x, [](int p, int q) { return (uint32_t)p > (uint32_t)q ? p : q; });
 }
 
 // A row's softmax, held by LPR lanes.
@@ -102,9 +112,7 @@ struct Row {
   float top, inv;                   // largest logit (0 for a row of none), 1 / sum of e
   bool some;                        // a head can be taken
   static __device__ __forceinline__ int head(int lane, int i) { return (i / V * LPR + lane) * V + i % V; }
-  __device__ __forceinline__ Row(const void* p, long long ld, long long row, bool live, int heads, int lane) {
-    float most = -INFINITY;
-    bool any = false;
+  __device__ __forceinline__ void load(const void* p, long long ld, long long row, bool live, int heads, int lane) {
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
       const int c = (j * LPR + lane) * V;
@@ -112,23 +120,17 @@ struct Row {
       for (int i = 0; i < V; ++i) x[j * V + i] = -INFINITY;
       if (live && c < heads) {
         float v[V];
-        load_n<V>((const T*)p + row * ld + c, heads - c, v);
+        ops::load_n<V>((const T*)p + row * ld + c, heads - c, v);
 #pragma unroll
         for (int i = 0; i < V; ++i) x[j * V + i] = c + i < heads ? v[i] : -INFINITY;
       }
     }
+  }
+  __device__ __forceinline__ void softmax() {
+    float most = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      any |= !(x[i] == -INFINITY);
-      most = fmaxf(most, x[i]);
-    }
-    int a = any;
-#pragma unroll
-    for (int o = LPR / 2; o; o >>= 1) {
-      most = fmaxf(most, __shfl_xor(most, o));
-      a |= __shfl_xor(a, o);
-    }
-    some = a != 0;
+    for (int i = 0; i < N; ++i) most = fmaxf(most, x[i]);
+    most = lanes_max<LPR>(most);
     top = most > -INFINITY ? most : 0.f;
     float s = 0.f;
 #pragma unroll
@@ -137,83 +139,106 @@ struct Row {
       s += e[i];
     }
     s = lanes_sum<LPR>(s);
+    some = !(s == 0.f);             // (1 at least, or NaN)
     inv = some ? 1.f / s : 0.f;
   }
 };
 
-// The totals of all blocks' (or one block's) sums: counts, share, loss.  red:
-// [blockDim.x] doubles.
-__device__ void totals(const GateArgs& a, int blocks, const float* pp, const int* pc, double* red) {
-  const int t = threadIdx.x, n = blockDim.x;
-  __shared__ int routed, chosen;
-  __shared__ double loss;
-  if (t == 0) { routed = 0; chosen = 0; }
-  __syncthreads();
-  int r = 0;
-  for (int b = t; b < blocks; b += n) r += pc[(size_t)b * (a.heads + 1) + a.heads];
-  if (r) atomicAdd(&routed, r);
-  // a head's partial sums in `slices` parts
-  int width = 1;
-  while (width < a.heads && width < n) width <<= 1;
-  const int slices = n / width, l = t & (width - 1), q = t / width;
-  double mine = 0.0;                // sum over this thread's heads of counts * sums of p
-  for (int h0 = 0; h0 < a.heads; h0 += width) {
-    const int h = h0 + l;
-    double p = 0.0;
-    int c = 0;
-    if (h < a.heads)
-      for (int b = q; b < blocks; b += slices) {
-        p += (double)pp[(size_t)b * a.heads + h];
-        c += pc[(size_t)b * (a.heads + 1) + h];
-      }
+// Counts, share and loss from a head's totals: thread t has heads t, t + n, ...
+// whose counts and sums of p are c[head], p[head].  red: [16] doubles, n_red [16].
+template <class P>
+__device__ __forceinline__ void finish(const GateArgs& a, const int* c, const P* p, int routed, double* red, int* n_red) {
+  double mine = 0.0;
+  int chosen = 0;
+  for (int h = threadIdx.x; h < a.heads; h += blockDim.x) {
+    const double share = routed ? (double)p[h] / routed : 0.0;
+    a.counts[h] = c[h];
+    a.share[h] = (float)share;
+    mine += share * c[h];
+    chosen += c[h];
+  }
+  // (up to 64 heads: the first wave has them all)
+#pragma unroll
+  for (int o = 32; o; o >>= 1) {
+    mine += __shfl_xor(mine, o);
+    chosen += __shfl_xor(chosen, o);
+  }
+  if (a.heads > 64) {
+    if ((threadIdx.x & 63) == 0) {
+      red[threadIdx.x >> 6] = mine;
+      n_red[threadIdx.x >> 6] = chosen;
+    }
     __syncthreads();
-    red[t] = p;
-    __syncthreads();
-    p = 0.0;
-    if (q == 0)
-      for (int k = 0; k < slices; ++k) p += red[k * width + l];
-    __syncthreads();
-    ((int*)red)[t] = c;
-    __syncthreads();
-    if (q == 0 && h < a.heads) {
-      c = 0;
-      for (int k = 0; k < slices; ++k) c += ((int*)red)[k * width + l];
-      a.counts[h] = c;
-      atomicAdd(&chosen, c);
-      const double share = routed ? p / routed : 0.0;
-      a.share[h] = (float)share;
-      mine += share * c;
+    mine = 0.0;
+    chosen = 0;
+    for (int w = 0; w < (int)blockDim.x / 64; ++w) {
+      mine += red[w];
+      chosen += n_red[w];
     }
   }
-  __syncthreads();
-  red[t] = mine;
-  __syncthreads();
-  if (t < 64) {
-    mine = 0.0;
-    for (int k = t; k < n; k += 64) mine += red[k];
-#pragma unroll
-    for (int o = 32; o; o >>= 1) mine += __shfl_xor(mine, o);
-    if (t == 0) {
-      a.counts[a.heads] = routed;
-      a.loss[0] = chosen ? (float)(mine * a.heads / chosen) : 0.f;
-    }
+  if (threadIdx.x == 0) {
+    a.counts[a.heads] = routed;
+    a.loss[0] = chosen ? (float)(mine * a.heads / chosen) : 0.f;
   }
 }
 
-__global__ void __launch_bounds__(1024) k_gate_fold(GateArgs a, int blocks) {
-  __shared__ double red[1024];
-  totals(a, blocks, a.part_p, a.part_c, red);
+// The blocks' partial rows added, in parts of the blocks side by side and those
+// in their order; then as above.
+__global__ void __launch_bounds__(1024) k_gate_fold(GateArgs a, int blocks, int width_bits) {
+  __shared__ double sum[HEADS + 1024], red[16];
+  __shared__ int cnt[HEADS + 1024], n_red[16];
+  const int t = threadIdx.x, width = 1 << width_bits, l = t & (width - 1), q = t >> width_bits, slices = 1024 >> width_bits;
+  // heads 0 .. heads - 1, then the rows that have a head
+  for (int h0 = 0; h0 <= a.heads; h0 += width) {
+    const int h = h0 + l;
+    double p = 0.0;
+    int c = 0;
+    if (h <= a.heads) {
+#pragma unroll 8
+      for (int b = q; b < blocks; b += slices) {
+        if (h < a.heads) p += (double)a.part_p[(size_t)b * a.heads + h];
+        c += a.part_c[(size_t)b * (a.heads + 1) + h];
+      }
+    }
+    for (int o = width; o < 64; o <<= 1) {
+      p += __shfl_xor(p, o);
+      c += __shfl_xor(c, o);
+    }
+    // (a wave's part, or several waves side by side where a part is wider)
+    const int parts = width < 64 ? 16 : slices, part = width < 64 ? t >> 6 : q;
+    __syncthreads();
+    if (width >= 64 || (t & 63) < width) {
+      sum[HEADS + part * width + l] = p;
+      cnt[HEADS + part * width + l] = c;
+    }
+    __syncthreads();
+    if (t < width && h <= a.heads) {
+      p = 0.0;
+      c = 0;
+      for (int k = 0; k < parts; ++k) {
+        p += sum[HEADS + k * width + l];
+        c += cnt[HEADS + k * width + l];
+      }
+      if (h < HEADS) sum[h] = p;
+      if (h == a.heads) n_red[0] = c;
+      else cnt[h] = c;
+    }
+  }
+  __syncthreads();
+  const int routed = n_red[0];
+  __syncthreads();
+  finish(a, cnt, sum, routed, red, n_red);
 }
 
 // MANY: more than KREG heads of a row.
 template <class T, int NJ, int LPR, bool MANY>
 __global__ void __launch_bounds__(1024) k_gate(GateArgs a) {
   typedef Row<T, NJ, LPR> R;
-  typedef Key<T> K;
   constexpr int N = R::N, ACROSS = LPR * N;
   // counts [heads + 1]; then the waves' sums of p, or the rows' keys
   extern __shared__ int lds[];
-  __shared__ double red[1024];
+  __shared__ double red[16];
+  __shared__ int n_red[16];
   int* cnt = lds;
   const int rpb = blockDim.x / LPR, lane = threadIdx.x % LPR, sub = threadIdx.x / LPR;
   uint32_t* keys = (uint32_t*)(lds + a.heads + 1) + sub * ACROSS;
@@ -223,10 +248,15 @@ __global__ void __launch_bounds__(1024) k_gate(GateArgs a) {
   for (int i = 0; i < N; ++i) sum[i] = 0.f;
   __syncthreads();
   int routed = 0;
-  for (long long r0 = (long long)blockIdx.x * rpb; r0 < a.rows; r0 += (long long)gridDim.x * rpb) {
+  const long long step = (long long)gridDim.x * rpb;
+  R next;
+  next.load(a.x, a.ldx, (long long)blockIdx.x * rpb + sub, (long long)blockIdx.x * rpb + sub < a.rows, a.heads, lane);
+  for (long long r0 = (long long)blockIdx.x * rpb; r0 < a.rows; r0 += step) {
     const long long row = r0 + sub;
     const bool live = row < a.rows;
-    const R r(a.x, a.ldx, row, live, a.heads, lane);
+    R r = next;
+    next.load(a.x, a.ldx, row + step, row + step < a.rows, a.heads, lane);
+    r.softmax();
     float* w = a.weights + row * a.k;
     int* id = a.indices + row * a.k;
     if (r.some) {
@@ -235,11 +265,12 @@ __global__ void __launch_bounds__(1024) k_gate(GateArgs a) {
       for (int i = 0; i < N; ++i) sum[i] += r.e[i] * r.inv;
     }
     if constexpr (!MANY) {
-      typename K::type key[N];
+      constexpr bool B16 = sizeof(T) == 2;
+      uint32_t key[N];
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const int h = R::head(lane, i);
-        key[i] = h < a.heads ? K::make(r.x[i], h) : 0;
+        key[i] = h >= a.heads ? 0u : B16 ? (ordered(r.x[i]) & 0xffff0000u) | (0xffffu - (uint32_t)h) : ordered(r.x[i]);
       }
       float ws[KREG];
       int is[KREG];
@@ -249,19 +280,28 @@ __global__ void __launch_bounds__(1024) k_gate(GateArgs a) {
         ws[s] = 0.f;
         is[s] = -1;
         if (s < a.k) {
-          typename K::type best = key[0];
+          uint32_t best = key[0];
 #pragma unroll
           for (int i = 1; i < N; ++i) best = key[i] > best ? key[i] : best;
+          best = lanes_max<LPR>(best);
+          int h;
+          if constexpr (B16) {
+            h = (int)(0xffffu - (best & 0xffffu));
 #pragma unroll
-          for (int o = LPR / 2; o; o >>= 1) {
-            const typename K::type other = __shfl_xor(best, o);
-            best = other > best ? other : best;
+            for (int i = 0; i < N; ++i) key[i] = key[i] == best ? 0u : key[i];
+            best &= 0xffff0000u;
+          } else {
+            // the lowest head of this key
+            uint32_t least = 0;
+#pragma unroll
+            for (int i = N - 1; i >= 0; --i) least = key[i] == best ? 0xffffu - (uint32_t)R::head(lane, i) : least;
+            h = (int)(0xffffu - lanes_max<LPR>(least));
+#pragma unroll
+            for (int i = 0; i < N; ++i) key[i] = R::head(lane, i) == h ? 0u : key[i];
           }
-#pragma unroll
-          for (int i = 0; i < N; ++i) key[i] = key[i] == best ? 0 : key[i];
-          const float x = K::value(best);
+          const float x = value_of(best, B16);
           if (!(x == -INFINITY)) {
-            is[s] = K::head(best);
+            is[s] = h;
             ws[s] = exp_of(x - r.top);
             total += ws[s];
           }
@@ -286,8 +326,7 @@ __global__ void __launch_bounds__(1024) k_gate(GateArgs a) {
         keys[h] = h < a.heads ? ordered(r.x[i]) : 0;
         places += !(r.x[i] == -INFINITY);
       }
-#pragma unroll
-      for (int o = LPR / 2; o; o >>= 1) places += __shfl_xor(places, o);
+      places = lanes_add<LPR>(places);
       __syncthreads();
       int rank[N];
 #pragma unroll
@@ -338,14 +377,12 @@ __global__ void __launch_bounds__(1024) k_gate(GateArgs a) {
     }
   __syncthreads();
   if (gridDim.x == 1) {
-    // (waves' sums as partial rows of p; the counts are whole)
     for (int h = threadIdx.x; h < a.heads; h += blockDim.x) {
       float s = 0.f;
       for (int k = 0; k < (int)blockDim.x / 64; ++k) s += waves[k * a.heads + h];
       waves[h] = s;
     }
-    __syncthreads();
-    totals(a, 1, waves, cnt, red);
+    finish(a, cnt, waves, cnt[a.heads], red, n_red);      // (a thread's heads are those that it added)
     return;
   }
   for (int h = threadIdx.x; h < a.heads; h += blockDim.x) {
@@ -354,6 +391,32 @@ __global__ void __launch_bounds__(1024) k_gate(GateArgs a) {
     a.part_p[(size_t)blockIdx.x * a.heads + h] = s;
   }
   for (int h = threadIdx.x; h <= a.heads; h += blockDim.x) a.part_c[(size_t)blockIdx.x * (a.heads + 1) + h] = cnt[h];
+}
+
+// Up to KREG values of a row's n choices, four or two at a time where they
+// come so.
+template <class S>
+__device__ __forceinline__ void load_choices(const S* p, int n, S* x, S none) {
+  typedef S four __attribute__((ext_vector_type(4), aligned(4)));
+  typedef S two __attribute__((ext_vector_type(2), aligned(4)));
+#pragma unroll
+  for (int s = 0; s < KREG; s += 4) {
+    if (n - s >= 4) {
+      const four v = *(const four*)(p + s);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[s + i] = v[i];
+    } else {
+      x[s] = x[s + 1] = x[s + 2] = x[s + 3] = none;
+      if (n - s >= 2) {
+        const two v = *(const two*)(p + s);
+        x[s] = v[0];
+        x[s + 1] = v[1];
+        if (n - s == 3) x[s + 2] = p[s + 2];
+      } else if (n - s == 1) {
+        x[s] = p[s];
+      }
+    }
+  }
 }
 
 // With p the softmax, f = counts / their sum and R the rows that have a head:
@@ -365,6 +428,18 @@ __global__ void __launch_bounds__(256) k_gate_bwd(GateArgs a) {
   typedef Row<T, NJ, LPR> R;
   constexpr int N = R::N, V = R::V;
   const int rpb = 256 / LPR, lane = threadIdx.x % LPR, sub = threadIdx.x / LPR;
+  const long long step = (long long)gridDim.x * rpb;
+  long long row = (long long)blockIdx.x * rpb + sub;
+  R next;
+  int ni[KREG];
+  float nd[KREG];
+  const auto ahead = [&](long long at) {
+    next.load(a.x, a.ldx, at, at < a.rows, a.heads, lane);
+    const int n = a.dw && at < a.rows ? a.k : 0;
+    load_choices(a.chosen + at * a.k, n, ni, -1);
+    load_choices(a.dw + at * a.k, n, nd, 0.f);
+  };
+  ahead(row);
   float f[N];
   int all = 0;
 #pragma unroll
@@ -373,42 +448,44 @@ __global__ void __launch_bounds__(256) k_gate_bwd(GateArgs a) {
     f[i] = (float)c;
     all += c;
   }
-#pragma unroll
-  for (int o = LPR / 2; o; o >>= 1) all += __shfl_xor(all, o);
+  all = lanes_add<LPR>(all);
   const int routed = a.n[a.heads];
   const float scale = all > 0 && routed > 0 ? (float)(a.balance * a.heads / ((double)routed * all)) : 0.f;
 #pragma unroll
   for (int i = 0; i < N; ++i) f[i] *= scale;
-  for (long long r0 = (long long)blockIdx.x * rpb; r0 < a.rows; r0 += (long long)gridDim.x * rpb) {
-    const long long row = r0 + sub;
+  for (long long r0 = (long long)blockIdx.x * rpb; r0 < a.rows; r0 += step, row += step) {
     const bool live = row < a.rows;
-    const R r(a.x, a.ldx, row, live, a.heads, lane);
+    R r = next;
+    int is[KREG];
+    float ds[KREG];
+#pragma unroll
+    for (int s = 0; s < KREG; ++s) {
+      is[s] = ni[s];
+      ds[s] = nd[s];
+    }
+    ahead(row + step);
     float d[N];
     uint32_t mark = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) d[i] = 0.f;
-    if (a.dw && live)
-      for (int s0 = 0; s0 < a.k; s0 += KREG) {
-        int is[KREG];
-        float ds[KREG];
-#pragma unroll
-        for (int s = 0; s < KREG; ++s) {
-          is[s] = -1;
-          ds[s] = 0.f;
-          if (s0 + s < a.k) {
-            is[s] = a.chosen[row * a.k + s0 + s];
-            ds[s] = a.dw[row * a.k + s0 + s];
-          }
-        }
-#pragma unroll
-        for (int s = 0; s < KREG; ++s)
-#pragma unroll
-          for (int i = 0; i < N; ++i)
-            if (is[s] == R::head(lane, i)) {
-              d[i] += ds[s];
-              mark |= 1u << i;
-            }
+    for (int s0 = 0; s0 < a.k; s0 += KREG) {
+      if (s0 > 0) {
+        const int n = a.dw && live ? a.k - s0 : 0;
+        load_choices(a.chosen + row * a.k + s0, n, is, -1);
+        load_choices(a.dw + row * a.k + s0, n, ds, 0.f);
       }
+#pragma unroll
+      for (int s = 0; s < KREG; ++s) {
+        if (s0 + s >= a.k) break;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+          if (is[s] == R::head(lane, i)) {
+            d[i] += ds[s];
+            mark |= 1u << i;
+          }
+      }
+    }
+    r.softmax();
     float dot = 0.f, dotw = 0.f, total = 0.f;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -476,7 +553,7 @@ void gate_grid(bool bf16, long long rows, int heads, int k, int& blocks, int& th
   blocks = 1;
   threads = many ? 256 : 1024;
   if (rows * lpr <= 2048) return;
-  if (rows * lpr <= 256LL * GATE_GRID) threads = 256;
+  if (rows * lpr <= 512LL * GATE_GRID) threads = 256;
   const long long n = (rows * lpr + threads - 1) / threads;
   blocks = (int)(n < GATE_GRID ? n : GATE_GRID);
 }
@@ -495,7 +572,11 @@ painn_status run_gate(painn_ctx* ctx, const GateArgs& a, int blocks, int threads
     if (many) k_gate<T, NJ, LPR, true><<<blocks, threads, lds, ctx->stream>>>(a);
     else k_gate<T, NJ, LPR, false><<<blocks, threads, lds, ctx->stream>>>(a);
   });
-  if (blocks > 1) k_gate_fold<<<1, 1024, 0, ctx->stream>>>(a, blocks);
+  if (blocks > 1) {
+    int bits = 0;                   // heads side by side, and the rows' count
+    while (bits < 10 && 1 << bits < a.heads + 1) ++bits;
+    k_gate_fold<<<1, 1024, 0, ctx->stream>>>(a, blocks, bits);
+  }
   prof_mark(ctx->prof, ctx->stream, KC_GATE, false);
   return launched(ctx, "gate launch");
 }
@@ -506,7 +587,7 @@ painn_status run_gate_bwd(painn_ctx* ctx, const GateArgs& a) {
   gate_form<T>(a.heads, [&](auto nj, auto lanes) {
     constexpr int NJ = decltype(nj)::value, LPR = decltype(lanes)::value;
     const long long n = (a.rows * LPR + 255) / 256;
-    k_gate_bwd<T, NJ, LPR><<<(unsigned)(n < 4096 ? n : 4096), 256, 0, ctx->stream>>>(a);
+    k_gate_bwd<T, NJ, LPR><<<(unsigned)(n < GATE_BWD ? n : GATE_BWD), 256, 0, ctx->stream>>>(a);
   });
   prof_mark(ctx->prof, ctx->stream, KC_GATE_BWD, false);
   return launched(ctx, "gate reverse launch");

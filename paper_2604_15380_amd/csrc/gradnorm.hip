@@ -27,7 +27,7 @@ namespace {
 
 using namespace ops;
 
-constexpr int PIECE = 8192, GRID = 1024, TB = 256;
+constexpr int PIECE = 8192, GRID = 2048, TB = 256;
 
 struct GradTensor {
   long long n;
@@ -84,17 +84,25 @@ __global__ void __launch_bounds__(TB) k_grad_squares(const GradTensor* __restric
   if (threadIdx.x == 0) part[blockIdx.x] = sum;
 }
 
-// result: the norm and the factor that takes it to max_norm at most.
-__global__ void __launch_bounds__(TB) k_grad_fold(const double* __restrict__ part, int n, double max_norm,
-                                                  float* __restrict__ result) {
+// The factor that takes the norm to max_norm at most, from the blocks' sums; the
+// block that is asked to writes result, the norm and the factor.
+__device__ __forceinline__ float factor_of(const double* __restrict__ part, int n, double max_norm, bool write,
+                                           float* __restrict__ result) {
   __shared__ double lds[TB / 64];
   double s = 0.0;
+#pragma unroll 8
   for (int k = threadIdx.x; k < n; k += TB) s += part[k];
   const double norm = sqrt(block_sum(s, lds));
-  if (threadIdx.x == 0) {
+  const float f = norm != norm ? (float)norm : norm > max_norm ? (float)(max_norm / norm) : 1.f;
+  if (write && threadIdx.x == 0) {
     result[0] = (float)norm;
-    result[1] = norm != norm ? (float)norm : norm > max_norm ? (float)(max_norm / norm) : 1.f;
+    result[1] = f;
   }
+  return f;
+}
+__global__ void __launch_bounds__(TB) k_grad_fold(const double* __restrict__ part, int n, double max_norm,
+                                                  float* __restrict__ result) {
+  factor_of(part, n, max_norm, true, result);
 }
 
 template <class T>
@@ -115,10 +123,13 @@ __device__ __forceinline__ void scale(const T* g, T* out, long long left, float 
   }
 }
 
+// Every block adds the sums by itself, in the same order: less than a launch in
+// between takes.
 __global__ void __launch_bounds__(TB) k_grad_scale(const GradTensor* __restrict__ tensors,
                                                    const Piece* __restrict__ pieces, long long n,
-                                                   const float* __restrict__ result) {
-  const float f = result[1];
+                                                   const double* __restrict__ part, int parts, double max_norm,
+                                                   float* __restrict__ result) {
+  const float f = factor_of(part, parts, max_norm, blockIdx.x == 0, result);
   for (long long k = blockIdx.x; k < n; k += gridDim.x) {
     const Piece c = pieces[k];
     const GradTensor t = tensors[c.tensor];
@@ -143,8 +154,10 @@ painn_status norm_of(painn_grad_norm* h, double max_norm, float* result, bool cl
   const int grid = (int)(h->pieces < GRID ? h->pieces : GRID);
   prof_mark(ctx->prof, ctx->stream, KC_GRAD_NORM, true);
   if (grid) k_grad_squares<<<grid, TB, 0, ctx->stream>>>(tt, pp, h->pieces, h->part);
-  k_grad_fold<<<1, TB, 0, ctx->stream>>>(h->part, grid, max_norm, result);
-  if (grid && clip) k_grad_scale<<<grid, TB, 0, ctx->stream>>>(tt, pp, h->pieces, result);
+  if (grid && clip)
+    k_grad_scale<<<grid, TB, 0, ctx->stream>>>(tt, pp, h->pieces, h->part, grid, max_norm, result);
+  else
+    k_grad_fold<<<1, TB, 0, ctx->stream>>>(h->part, grid, max_norm, result);
   prof_mark(ctx->prof, ctx->stream, KC_GRAD_NORM, false);
   return launched(ctx, "gradient norm launch");
 }

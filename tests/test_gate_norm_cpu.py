@@ -57,7 +57,7 @@ def test_workspace_sizes():
     gate = binding.painn_gate_workspace
     assert gate(1, 200, 16, 2) == 0 and gate(2, 0, 16, 2) == 0
     for rows in (10**5, 2**31 - 1):
-        assert 0 < gate(1, rows, 64, 2) <= 256 * (64 + 65) * 4 + 512
+        assert 0 < gate(1, rows, 64, 2) <= 512 * (64 + 65) * 4 + 512
 
 
 def runtime():
