@@ -14,7 +14,7 @@
 
 #include <type_traits>
 
-#include "ops.h"
+#include "raw.h"
 
 namespace {
 
@@ -112,22 +112,24 @@ struct Row {
   float top, inv;                   // largest logit (0 for a row of none), 1 / sum of e
   bool some;                        // a head can be taken
   static __device__ __forceinline__ int head(int lane, int i) { return (i / V * LPR + lane) * V + i % V; }
+  Raw<T, V> raw[NJ];
+  // (the values stay on their way until softmax)
   __device__ __forceinline__ void load(const void* p, long long ld, long long row, bool live, int heads, int lane) {
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
       const int c = (j * LPR + lane) * V;
-#pragma unroll
-      for (int i = 0; i < V; ++i) x[j * V + i] = -INFINITY;
-      if (live && c < heads) {
-        float v[V];
-        ops::load_n<V>((const T*)p + row * ld + c, heads - c, v);
-#pragma unroll
-        for (int i = 0; i < V; ++i) x[j * V + i] = c + i < heads ? v[i] : -INFINITY;
-      }
+      raw[j] = zero_raw<T, V>();
+      if (live && c < heads) raw[j] = load_raw<T, V, false>((const T*)p + row * ld + c, heads - c);
     }
   }
-  __device__ __forceinline__ void softmax() {
+  __device__ __forceinline__ void softmax(bool live, int heads, int lane) {
     float most = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      unpack<T, V>(raw[j], x + j * V);
+#pragma unroll
+      for (int i = 0; i < V; ++i) x[j * V + i] = live && head(lane, j * V + i) < heads ? x[j * V + i] : -INFINITY;
+    }
 #pragma unroll
     for (int i = 0; i < N; ++i) most = fmaxf(most, x[i]);
     most = lanes_max<LPR>(most);
@@ -256,7 +258,7 @@ __global__ void __launch_bounds__(1024) k_gate(GateArgs a) {
     const bool live = row < a.rows;
     R r = next;
     next.load(a.x, a.ldx, row + step, row + step < a.rows, a.heads, lane);
-    r.softmax();
+    r.softmax(live, a.heads, lane);
     float* w = a.weights + row * a.k;
     int* id = a.indices + row * a.k;
     if (r.some) {
@@ -485,7 +487,7 @@ __global__ void __launch_bounds__(256) k_gate_bwd(GateArgs a) {
           }
       }
     }
-    r.softmax();
+    r.softmax(live, a.heads, lane);
     float dot = 0.f, dotw = 0.f, total = 0.f;
 #pragma unroll
     for (int i = 0; i < N; ++i) {

@@ -11,15 +11,14 @@
 #include <new>
 #include <vector>
 
-#include "ops.h"
+#include "raw.h"
 
 struct painn_grad_norm {
   painn_ctx* ctx = nullptr;       // null: the context has been destroyed
   painn_grad_norm *prev = nullptr, *next = nullptr;  // of the context's
   long long pieces = 0;
   bool outs = true;               // every tensor has a place for its clipped values
-  void* table = nullptr;          // GradTensor [n_tensors], Piece [pieces], double [GRID]
-  const void* piece_list = nullptr;
+  void* table = nullptr;          // Piece [pieces], double [GRID]
   double* part = nullptr;
 };
 
@@ -29,14 +28,11 @@ using namespace ops;
 
 constexpr int PIECE = 8192, GRID = 2048, TB = 256;
 
-struct GradTensor {
-  long long n;
+// Up to 8,192 consecutive values of a tensor.
+struct Piece {
   const void* g;
   void* out;
-  int bf16, unused;
-};
-struct Piece {
-  int tensor, index;              // values [8192 index, 8192 (index + 1)) of the tensor
+  int n, bf16;
 };
 
 __device__ __forceinline__ double block_sum(double s, double* lds) {
@@ -50,35 +46,49 @@ __device__ __forceinline__ double block_sum(double s, double* lds) {
   return s;
 }
 
+// A thread's values of a piece: all loads first.
 template <class T>
-__device__ __forceinline__ void add_squares(const T* g, long long left, double* s) {
-  constexpr int V = 16 / sizeof(T), STEPS = PIECE / (TB * V);
-  float x[STEPS][V];
+struct Part {
+  static constexpr int V = 16 / sizeof(T), STEPS = PIECE / (TB * V);
+  Raw<T, V> r[STEPS];
+  static __device__ __forceinline__ int at(int j) { return (j * TB + (int)threadIdx.x) * V; }
+  __device__ __forceinline__ Part(const T* g, int n) {
+    if (n == PIECE) {
 #pragma unroll
-  for (int j = 0; j < STEPS; ++j) {
-    const int at = (j * TB + (int)threadIdx.x) * V;
-    load_n<V>(g + at, left - at, x[j]);
+      for (int j = 0; j < STEPS; ++j) r[j] = load_raw<T, V, true>(g + at(j), V);
+    } else {
+#pragma unroll
+      for (int j = 0; j < STEPS; ++j) r[j] = at(j) < n ? load_raw<T, V, false>(g + at(j), n - at(j)) : zero_raw<T, V>();
+    }
   }
+};
+
+template <class T>
+__device__ __forceinline__ void add_squares(const T* g, int n, double* s) {
+  typedef Part<T> P;
+  const P p(g, n);
 #pragma unroll
-  for (int j = 0; j < STEPS; ++j)
+  for (int j = 0; j < P::STEPS; ++j) {
+    float x[P::V];
+    unpack<T, P::V>(p.r[j], x);
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const double d = (double)x[j][i];
+    for (int i = 0; i < P::V; ++i) {
+      const double d = (double)x[i];
       s[i & 1] = __builtin_fma(d, d, s[i & 1]);
     }
+  }
 }
 
-__global__ void __launch_bounds__(TB) k_grad_squares(const GradTensor* __restrict__ tensors,
-                                                     const Piece* __restrict__ pieces, long long n,
+__global__ void __launch_bounds__(TB) k_grad_squares(const Piece* __restrict__ pieces, long long n,
                                                      double* __restrict__ part) {
   __shared__ double lds[TB / 64];
   double s[2] = {0.0, 0.0};
+  Piece next = pieces[blockIdx.x];          // (there are as many pieces as blocks at least)
   for (long long k = blockIdx.x; k < n; k += gridDim.x) {
-    const Piece c = pieces[k];
-    const GradTensor t = tensors[c.tensor];
-    const long long at = (long long)c.index * PIECE;
-    if (t.bf16) add_squares((const b16*)t.g + at, t.n - at, s);
-    else add_squares((const float*)t.g + at, t.n - at, s);
+    const Piece c = next;
+    if (k + gridDim.x < n) next = pieces[k + gridDim.x];
+    if (c.bf16) add_squares((const b16*)c.g, c.n, s);
+    else add_squares((const float*)c.g, c.n, s);
   }
   const double sum = block_sum(s[0] + s[1], lds);
   if (threadIdx.x == 0) part[blockIdx.x] = sum;
@@ -106,37 +116,34 @@ __global__ void __launch_bounds__(TB) k_grad_fold(const double* __restrict__ par
 }
 
 template <class T>
-__device__ __forceinline__ void scale(const T* g, T* out, long long left, float f) {
-  constexpr int V = 16 / sizeof(T), STEPS = PIECE / (TB * V);
-  float x[STEPS][V];
+__device__ __forceinline__ void scale(const T* g, T* out, int n, float f) {
+  typedef Part<T> P;
+  const P p(g, n);
 #pragma unroll
-  for (int j = 0; j < STEPS; ++j) {
-    const int at = (j * TB + (int)threadIdx.x) * V;
-    load_n<V>(g + at, left - at, x[j]);
-  }
+  for (int j = 0; j < P::STEPS; ++j) {
+    float x[P::V];
+    unpack<T, P::V>(p.r[j], x);
 #pragma unroll
-  for (int j = 0; j < STEPS; ++j) {
-    const int at = (j * TB + (int)threadIdx.x) * V;
-#pragma unroll
-    for (int i = 0; i < V; ++i) x[j][i] *= f;
-    store_n<V>(out + at, left - at, x[j]);
+    for (int i = 0; i < P::V; ++i) x[i] *= f;
+    if (n == PIECE) store<P::V>(out + P::at(j), x);
+    else store_n<P::V>(out + P::at(j), n - P::at(j), x);
   }
 }
 
 // Every block adds the sums by itself, in the same order: less than a launch in
-// between takes.
-__global__ void __launch_bounds__(TB) k_grad_scale(const GradTensor* __restrict__ tensors,
-                                                   const Piece* __restrict__ pieces, long long n,
+// between takes, and than a count of the blocks that have ended (67 M values: 14
+// us for its 2,048 atomic additions).
+__global__ void __launch_bounds__(TB) k_grad_scale(const Piece* __restrict__ pieces, long long n,
                                                    const double* __restrict__ part, int parts, double max_norm,
                                                    float* __restrict__ result) {
+  Piece next = pieces[blockIdx.x];
   const float f = factor_of(part, parts, max_norm, blockIdx.x == 0, result);
   for (long long k = blockIdx.x; k < n; k += gridDim.x) {
-    const Piece c = pieces[k];
-    const GradTensor t = tensors[c.tensor];
-    if (f == 1.f && t.out == t.g) continue;
-    const long long at = (long long)c.index * PIECE;
-    if (t.bf16) scale((const b16*)t.g + at, (b16*)t.out + at, t.n - at, f);
-    else scale((const float*)t.g + at, (float*)t.out + at, t.n - at, f);
+    const Piece c = next;
+    if (k + gridDim.x < n) next = pieces[k + gridDim.x];
+    if (f == 1.f && c.out == c.g) continue;
+    if (c.bf16) scale((const b16*)c.g, (b16*)c.out, c.n, f);
+    else scale((const float*)c.g, (float*)c.out, c.n, f);
   }
 }
 
@@ -149,15 +156,12 @@ painn_status norm_of(painn_grad_norm* h, double max_norm, float* result, bool cl
   if (clip && !h->outs) return fail(ctx, PAINN_E_ARG, "a tensor has no place for its clipped values");
   (void)hipSetDevice(ctx->device);
   (void)hipGetLastError();
-  const GradTensor* tt = (const GradTensor*)h->table;
-  const Piece* pp = (const Piece*)h->piece_list;
+  const Piece* pp = (const Piece*)h->table;
   const int grid = (int)(h->pieces < GRID ? h->pieces : GRID);
   prof_mark(ctx->prof, ctx->stream, KC_GRAD_NORM, true);
-  if (grid) k_grad_squares<<<grid, TB, 0, ctx->stream>>>(tt, pp, h->pieces, h->part);
-  if (grid && clip)
-    k_grad_scale<<<grid, TB, 0, ctx->stream>>>(tt, pp, h->pieces, h->part, grid, max_norm, result);
-  else
-    k_grad_fold<<<1, TB, 0, ctx->stream>>>(h->part, grid, max_norm, result);
+  if (grid) k_grad_squares<<<grid, TB, 0, ctx->stream>>>(pp, h->pieces, h->part);
+  if (grid && clip) k_grad_scale<<<grid, TB, 0, ctx->stream>>>(pp, h->pieces, h->part, grid, max_norm, result);
+  else k_grad_fold<<<1, TB, 0, ctx->stream>>>(h->part, grid, max_norm, result);
   prof_mark(ctx->prof, ctx->stream, KC_GRAD_NORM, false);
   return launched(ctx, "gradient norm launch");
 }
@@ -220,27 +224,26 @@ painn_status painn_grad_norm_create(painn_ctx* ctx, int32_t n_tensors, const pai
     ctx->grad_norms = h;
     h->pieces = pieces;
     h->outs = outs;
-    const size_t head = align256((size_t)n_tensors * sizeof(GradTensor));
-    const size_t body = align256((size_t)pieces * sizeof(Piece)), bytes = head + body;
-    std::vector<unsigned char> host(bytes);
-    GradTensor* ht = (GradTensor*)host.data();
-    Piece* hp = (Piece*)(host.data() + head);
+    const size_t list = align256((size_t)pieces * sizeof(Piece)), bytes = list + GRID * sizeof(double);
+    std::vector<unsigned char> host(list);
+    Piece* hp = (Piece*)host.data();
     for (int k = 0; k < n_tensors; ++k) {
       const painn_grad_tensor& t = tensors[k];
-      ht[k] = GradTensor{t.n, t.grad, t.out, t.precision == PAINN_BF16, 0};
-      for (long long i = 0; i * PIECE < t.n; ++i) *hp++ = Piece{k, (int)i};
+      const int size = t.precision == PAINN_BF16 ? 2 : 4;
+      for (int64_t i = 0; i < t.n; i += PIECE)
+        *hp++ = Piece{(const char*)t.grad + i * size, t.out ? (char*)t.out + i * size : nullptr,
+                      (int)(t.n - i < PIECE ? t.n - i : PIECE), t.precision == PAINN_BF16};
     }
     (void)hipSetDevice(ctx->device);
-    hipError_t e = hipMalloc(&h->table, bytes + GRID * sizeof(double));
-    if (e == hipSuccess && bytes) e = hipMemcpyAsync(h->table, host.data(), bytes, hipMemcpyHostToDevice, ctx->stream);
+    hipError_t e = hipMalloc(&h->table, bytes);
+    if (e == hipSuccess && list) e = hipMemcpyAsync(h->table, host.data(), list, hipMemcpyHostToDevice, ctx->stream);
     if (e == hipSuccess) e = hipStreamSynchronize(ctx->stream);
     if (e != hipSuccess) {
       (void)hipGetLastError();
       painn_grad_norm_free(h);
       return fail(ctx, PAINN_E_OOM, std::string("gradient table: ") + hipGetErrorString(e));
     }
-    h->piece_list = (const char*)h->table + head;
-    h->part = (double*)((char*)h->table + bytes);
+    h->part = (double*)((char*)h->table + list);
   } catch (...) {
     if (h) painn_grad_norm_free(h);
     return fail(ctx, PAINN_E_OOM, "host allocation failed");
