@@ -192,7 +192,7 @@ template <class T, int V, bool FULL, int ACT, int TB>
 __global__ void __launch_bounds__(TB) k_group_norm_bwd_tiles(GnArgs a) {
   __shared__ double lds[2 * TB];
   typedef Grads<T, V, FULL, ACT> G;
-  const int slab = blockIdx.x, t = blockIdx.y;
+  const int slab = blockIdx.x, t = (int)(gridDim.y - 1 - blockIdx.y);   // (the rows read last are in the caches)
   const Place<V> p(a, slab, threadIdx.x, TB);
   long_samples(a, t, [&](int, int sample, const Span& q, long long lo, long long hi) {
     double s[2];

@@ -508,8 +508,8 @@ class Runtime:
         if out is None:
             out = x.new_empty((n, c))
         py, ldy = self._rows(out, "out", x.dtype, n, c)
-        stats = x.new_empty((2, samples, groups), dtype=torch.float32)
-        mean, rstd = stats.unbind()
+        mean = x.new_empty((samples, groups), dtype=torch.float32)
+        rstd = torch.empty_like(mean)
         longest = max_rows or 0
         need = B.painn_group_norm_workspace(prec, n, c, groups, samples, each, longest, False)
         ws = x.new_empty(need, dtype=torch.uint8) if need else None
@@ -518,7 +518,7 @@ class Runtime:
             prec, act, n, c, groups, po, each, samples, 0, longest, eps, px, ldx, pw, pb, py, ldy, mean.data_ptr(),
             rstd.data_ptr(), ws.data_ptr() if need else 0, need))
         if cur is not None:
-            self._leave(cur, (x, weight, bias, offsets, out, stats, ws))
+            self._leave(cur, (x, weight, bias, offsets, out, mean, rstd, ws))
         return out, mean, rstd
 
     def group_norm_backward(self, dy, x, weight, bias, mean, rstd, groups, offsets=None, sample_rows=None,
@@ -564,17 +564,17 @@ class Runtime:
         if not 0 < k <= h:
             raise ValueError(f"k must be within 1 and {h} heads, not {k}")
         px, ldx = self._rows(logits, "logits", logits.dtype, n, h)
-        new = lambda *s, dtype=torch.float32: logits.new_empty(s, dtype=dtype)  # noqa: E731
-        weights, indices, sums, totals = new(n, k), new(n, k, dtype=torch.int32), new(h + 1), new(h + 1, dtype=torch.int32)
-        share, loss = sums[:h], sums[h]
+        f32, i32, new = torch.float32, torch.int32, logits.new_empty
+        weights, indices = new((n, k), dtype=f32), new((n, k), dtype=i32)
+        share, loss, totals = new((h,), dtype=f32), new((), dtype=f32), new((h + 1,), dtype=i32)
         need = B.painn_gate_workspace(prec, n, h, k)
-        ws = new(need, dtype=torch.uint8) if need else None
-        at = sums.data_ptr()
+        ws = new((need,), dtype=torch.uint8) if need else None
         cur = self._enter()
         B.painn_gate(self.ctx, B.gate_args(prec, h, n, k, bool(normalize), px, ldx, weights.data_ptr(), indices.data_ptr(),
-                                           totals.data_ptr(), at, at + 4 * h, ws.data_ptr() if need else 0, need))
+                                           totals.data_ptr(), share.data_ptr(), loss.data_ptr(),
+                                           ws.data_ptr() if need else 0, need))
         if cur is not None:
-            self._leave(cur, (logits, weights, indices, sums, totals, ws))
+            self._leave(cur, (logits, weights, indices, share, loss, totals, ws))
         return Gate(weights, indices, totals[:h], share, loss, totals, bool(normalize))
 
     def gate_backward(self, dweights, logits, gate, balance=0.0, dlogits=None):
