@@ -377,8 +377,9 @@ typedef enum {
  * non-decreasing within [0, rows]; entries outside are taken as the nearest
  * bound), or with offsets NULL [s sample_rows, (s+1) sample_rows), rows =
  * n_samples sample_rows.  A sample may be empty: its mean and rstd are 0.  Rows
- * of no sample are not written.  The sums of a set are formed in FP64 (forward)
- * or in FP32 for a few rows and FP64 beyond (reverse). */
+ * of no sample are not written.  The sums of a set are formed about a value near
+ * its mean, in FP32, or FP64 where that would lose digits (forward), or in FP32
+ * for a few values and FP64 beyond (reverse). */
 typedef struct {
   int32_t precision, activation;
   int64_t rows;

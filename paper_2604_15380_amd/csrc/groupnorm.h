@@ -32,7 +32,7 @@ struct GnArgs {
   int l_blocks, f_blocks;           // blocks of long and of other samples per slab; the tiles' blocks follow
   long long limit;                  // rows that a team takes on
   int tile, tiles;                  // rows of a tile, tiles (0: no sample is longer than limit)
-  double2* seg;                     // [tiles][2][groups] sums
+  double2* seg;                     // [tiles][2][groups]: mean and squares about it; the reverse pass's sums
   float* part;                      // [l_blocks + f_blocks + tiles][2][cols] column sums of the reverse pass, or null
 };
 
@@ -150,7 +150,10 @@ struct Rows {
     rows = p.rows;
     n = (int)count;
   }
-  __device__ __forceinline__ bool has(int i) const { return (FULL || left > 0) && row + i * rows < n; }
+  // (unsigned: row + i rows may pass 2^31 where a sample ends just below it)
+  __device__ __forceinline__ bool has(int i) const {
+    return (FULL || left > 0) && (uint32_t)row + (uint32_t)i * (uint32_t)rows < (uint32_t)n;
+  }
   __device__ __forceinline__ Raw<T, V> get(int i) const {
     if (has(i)) return load_raw<T, V, FULL>(at + i * step, left);
     return zero_raw<T, V>();
@@ -257,18 +260,24 @@ __device__ __forceinline__ void long_samples(const GnArgs& a, int t, F&& f) {
   }
 }
 
-// A long sample's sums: of its tiles, in an order that depends on the sample
-// alone.
-__device__ __forceinline__ void tiles_sum(const GnArgs& a, const Span& p, int group, int lane, int lanes, double* s) {
-  s[0] = s[1] = 0.0;
+// Calls f(sums, rows) for a long sample's tiles that fall to this one of `lanes`
+// lanes, in an order that depends on the sample alone.
+template <class F>
+__device__ __forceinline__ void each_tile(const GnArgs& a, const Span& p, int group, int lane, int lanes, F&& f) {
   if (group >= a.groups) return;
   const int from = (int)((uint32_t)p.a / (uint32_t)a.tile), to = (int)((uint32_t)(p.b - 1) / (uint32_t)a.tile);
   for (int u = from + lane; u <= to; u += lanes) {
-    const int slot = u == from && p.a != (long long)from * a.tile;
-    const double2 v = a.seg[((size_t)u * 2 + slot) * a.groups + group];
+    const long long lo = (long long)u * a.tile, hi = lo + a.tile;
+    const int slot = u == from && p.a != lo;
+    f(a.seg[((size_t)u * 2 + slot) * a.groups + group], (hi < p.b ? hi : p.b) - (lo > p.a ? lo : p.a));
+  }
+}
+__device__ __forceinline__ void tiles_sum(const GnArgs& a, const Span& p, int group, int lane, int lanes, double* s) {
+  s[0] = s[1] = 0.0;
+  each_tile(a, p, group, lane, lanes, [&](double2 v, long long) {
     s[0] += v.x;
     s[1] += v.y;
-  }
+  });
 }
 
 // ---- the plan -----------------------------------------------------------------------
@@ -323,6 +332,7 @@ inline Plan plan_of(bool bf16, long long rows, int cols, int groups, int samples
   long long room = LAUNCH_THREADS / 1024 / p.slabs - p.tiles;
   if (room > 65535 - p.tiles) room = 65535 - p.tiles;             // (the grid's second axis)
   if (backward && room > BLOCKS_BWD) room = BLOCKS_BWD;
+  if (room < 2) room = 2;                                         // (refused: more blocks than a launch holds)
   if (p.tb == 64 && ragged) {        // (a few where the caller says that there are none)
     room = (room + 1) / 2;
     const long long most = longest > p.team / lpr * 8 ? room : 8;

@@ -1,18 +1,18 @@
 // Group norm with an activation, channels last, over the rows of ragged samples,
 // and its reverse pass (FP32, BF16).
 //
-// A set is a sample's rows times a group's columns.  Its statistics come from
-// the sums of x and x^2 in FP64, so that neither the order nor a mean far from
-// 0 costs digits; the reverse pass takes the sums of a and a xh.  Bound by
+// A set is a sample's rows times a group's columns.  Its statistics are sums
+// about a value near its mean (FP32, or FP64 where that loses digits), so that a
+// mean far from 0 costs none; the reverse pass takes the sums of a and a xh.  Bound by
 // memory: x (and dy) should be read once.  A team of threads therefore holds a
 // sample's rows of one slab (whole groups, 128 bytes or more of a row, so that
 // no line is read by two teams) in registers between its sums and its result;
 // rows past those are read again.  How many threads a team has goes by the
-// samples' usual length, from a few lanes to a block of 1,024.
+// samples' usual length, from a few lanes to a block of 512.
 //
 // Samples longer than `limit` would leave the chip to a few teams.  They are
 // cut into tiles of R <= limit rows: the tiles' sums are formed by further
-// blocks of the first launch, and a second launch adds a sample's tiles, in
+// blocks of the first launch in FP64, and a second launch adds a sample's tiles, in
 // their order, and writes its result.  A tile meets at most two such samples,
 // the ones that hold its first and its last row, which gives every (tile,
 // sample) its place without a list.
@@ -21,38 +21,40 @@
 namespace {
 
 // ---- forward --------------------------------------------------------------------
-// FP64 sums of x and x^2.
-template <class T, int V>
-__device__ __forceinline__ void add_raw(const Raw<T, V>& r, double* s) {
-  float x[V];
-  unpack<T, V>(r, x);
-#pragma unroll
-  for (int i = 0; i < V; ++i) {
-    const double d = (double)x[i];
-    s[0] += d;
-    s[1] = __builtin_fma(d, d, s[1]);
-  }
-}
+// FP64 sums of x - pivot and its square.
 template <class T, int V, bool FULL, int U>
-__device__ __forceinline__ void add_rows(const Rows<T, V, FULL>& x, int from, double* s) {
-  for (int i0 = from; x.row + i0 * x.rows < x.n; i0 += U) {
+__device__ __forceinline__ void add_rows(const Rows<T, V, FULL>& x, float pivot, double* s) {
+  for (int i0 = 0; x.has(i0); i0 += U) {
     Raw<T, V> v[U];
 #pragma unroll
     for (int i = 0; i < U; ++i) v[i] = x.get(i0 + i);
 #pragma unroll
-    for (int i = 0; i < U; ++i) add_raw<T, V>(v[i], s);
+    for (int i = 0; i < U; ++i) {
+      float u[V];
+      unpack<T, V>(v[i], u);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const double d = x.has(i0 + i) && (FULL || e < x.left) ? (double)u[e] - (double)pivot : 0.0;
+        s[0] += d;
+        s[1] = __builtin_fma(d, d, s[1]);
+      }
+    }
   }
 }
+// The pivot of FP64 sums: the group's first value in a row, so that equal values
+// leave no squares (0 where it is not finite).
+template <class T, int V>
+__device__ __forceinline__ float first_value(const GnArgs& a, const Place<V>& p, long long row) {
+  float k = 0.f;
+  if (p.left > 0) load_n<1>((const T*)a.x + row * a.ldx + (long long)p.group * a.cg, 1, &k);
+  return fabsf(k) < INFINITY ? k : 0.f;
+}
 
-// mean and rstd from a set's FP64 sums over n values
-__device__ __forceinline__ void statistics(const GnArgs& a, const double* s, double n, float& mu, float& rs) {
-  const double m = s[0] / n;
-  double var = s[1] / n - m * m;
+// 1 / sqrt(variance + eps); what leaves FP32's range may have a root within it
+__device__ __forceinline__ float rstd_of(const GnArgs& a, double var) {
   if (var < 0.0) var = 0.0;
   var += (double)a.eps;
-  mu = (float)m;
-  // (a variance past FP32's range has a root within it)
-  rs = var < 1e38 ? 1.f / sqrtf((float)var) : (float)(1.0 / sqrt(var));
+  return var > 1e-30 && var < 1e38 ? 1.f / sqrtf((float)var) : (float)(1.0 / sqrt(var));
 }
 
 // d = x - pivot, 0 past the group's end, and the sums of d and d^2
@@ -85,8 +87,10 @@ __device__ __forceinline__ void normalise(const GnArgs& a, const Rows<T, V, FULL
 // sample's rows, in FP32:
 //   mean = K + sum d / n,  variance = sum d^2 / n - (sum d / n)^2.
 // With K the held rows' own mean the subtraction takes at most n / (held
-// values) times the sums' rounding, whatever the mean.  Squares that leave
-// FP32's range are formed again in FP64.
+// values) times the sums' rounding, whatever the mean.  The sums are formed again
+// in FP64 where that is not enough: squares that leave FP32's range, a
+// mean further from K than the deviation (rows held that say little of the rest;
+// equal values, K off by a rounding), a sample far longer than max_rows says.
 template <class T, int V, bool FULL, int ACT, int TB, bool REST>
 __device__ __forceinline__ void team_forward(const GnArgs& a, const Place<V>& p, int team, int s, const Span& q, double* lds) {
   constexpr int NR = steps_held(TB);
@@ -120,20 +124,25 @@ __device__ __forceinline__ void team_forward(const GnArgs& a, const Place<V>& p,
   }
   team_sum<TB, 2>(a, sum, team, flds);
   float mu = 0.f, rs = 0.f;
+  bool wild = false;
   const float count = (float)x.n * (float)a.cg;
   if (x.n > 0) {
     const float inv = __builtin_amdgcn_rcpf(count), d = sum[0] * inv, var = sum[1] * inv - d * d;
     const float ve = (var > 0.f || var != var ? var : 0.f) + a.eps;
     mu = pivot + d;
-    // (both to one step; below the range that the instruction keeps, the exact way)
-    rs = ve < 1e-36f ? 1.f / sqrtf(ve) : __builtin_amdgcn_rsqf(ve);
+    rs = __builtin_amdgcn_rsqf(ve);         // (to one step)
+    wild = !(sum[1] < 1e38f) || d * d > ve || ve < 1e-30f || (REST && (x.n >> 10) >= NR * p.rows);
   }
-  const bool wild = x.n > 0 && !(sum[1] < 1e38f);
   if (team_any<TB>(wild)) {
     double t[2] = {0.0, 0.0};
-    add_rows<T, V, FULL, 4>(x, 0, t);
+    const float k = x.n > 0 ? first_value<T, V>(a, p, q.a) : 0.f;
+    add_rows<T, V, FULL, 4>(x, k, t);
     team_sum<TB, 2>(a, t, team, lds);
-    if (wild) statistics(a, t, (double)x.n * a.cg, mu, rs);
+    if (wild) {
+      const double n = (double)x.n * a.cg, d = t[0] / n;
+      mu = (float)((double)k + d);
+      rs = rstd_of(a, t[1] / n - d * d);
+    }
   }
   if (s >= 0 && p.row == 0 && p.left == a.cg) {
     if (a.mean) a.mean[(size_t)s * a.groups + p.group] = mu;
@@ -171,9 +180,13 @@ __global__ void __launch_bounds__(TB) k_group_norm(GnArgs a) {
     const Place<V> p(a, slab, threadIdx.x, TB);
     long_samples(a, t, [&](int slot, int, const Span&, long long lo, long long hi) {
       double s[2] = {0.0, 0.0};
-      add_rows<T, V, FULL, 8>(Rows<T, V, FULL>(a.x, a.ldx, p, lo, hi - lo), 0, s);
+      // the part's mean, and the squares about it
+      const float k = first_value<T, V>(a, p, lo);
+      add_rows<T, V, FULL, 8>(Rows<T, V, FULL>(a.x, a.ldx, p, lo, hi - lo), k, s);
       team_sum<TB, 2>(a, s, TB, lds);
-      if (p.row == 0 && p.left == a.cg) a.seg[((size_t)t * 2 + slot) * a.groups + p.group] = make_double2(s[0], s[1]);
+      const double n = (double)(hi - lo) * a.cg, d = s[0] / n;
+      if (p.row == 0 && p.left == a.cg)
+        a.seg[((size_t)t * 2 + slot) * a.groups + p.group] = make_double2((double)k + d, s[1] - s[0] * d);
     });
     return;
   }
@@ -205,11 +218,18 @@ __global__ void __launch_bounds__(TB) k_group_norm_tiles(GnArgs a) {
   const int slab = blockIdx.x, t = (int)(gridDim.y - 1 - blockIdx.y);   // (the rows read last are in the caches)
   const Place<V> p(a, slab, threadIdx.x, TB);
   long_samples(a, t, [&](int, int sample, const Span& q, long long lo, long long hi) {
-    double s[2];
-    tiles_sum(a, q, p.group, p.row * a.lpg + (threadIdx.x & (a.lpg - 1)), p.rows * a.lpg, s);
-    team_sum<TB, 2>(a, s, TB, lds);
-    float mu, rs;
-    statistics(a, s, (double)(q.b - q.a) * a.cg, mu, rs);
+    // the parts' means and squares n, m, S: m = sum n m / N, then S + n (m - mean)^2
+    const double n = (double)(q.b - q.a) * a.cg;
+    double mean = 0.0, squares = 0.0;
+    const int lane = p.row * a.lpg + (threadIdx.x & (a.lpg - 1)), lanes = p.rows * a.lpg;
+    each_tile(a, q, p.group, lane, lanes, [&](double2 v, long long part) { mean += v.x * ((double)part * a.cg); });
+    team_sum<TB, 1>(a, &mean, TB, lds);
+    mean /= n;
+    each_tile(a, q, p.group, lane, lanes, [&](double2 v, long long part) {
+      squares += v.y + (v.x - mean) * (v.x - mean) * ((double)part * a.cg);
+    });
+    team_sum<TB, 1>(a, &squares, TB, lds);
+    const float mu = (float)mean, rs = rstd_of(a, squares / n);
     if (lo == q.a && p.row == 0 && p.left == a.cg) {
       if (a.mean) a.mean[(size_t)sample * a.groups + p.group] = mu;
       if (a.rstd) a.rstd[(size_t)sample * a.groups + p.group] = rs;
