@@ -555,7 +555,8 @@ void gate_grid(bool bf16, long long rows, int heads, int k, int& blocks, int& th
   blocks = 1;
   threads = many ? 256 : 1024;
   if (rows * lpr <= 2048) return;
-  if (rows * lpr <= 512LL * GATE_GRID) threads = 256;
+  // (65,502 x 16 BF16: half the partial rows of blocks of 256, whose fold took 8.0 us for 5.5)
+  if (rows * lpr <= 512LL * GATE_GRID) threads = many ? 256 : 512;
   const long long n = (rows * lpr + threads - 1) / threads;
   blocks = (int)(n < GATE_GRID ? n : GATE_GRID);
 }

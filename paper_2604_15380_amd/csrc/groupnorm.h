@@ -12,7 +12,10 @@ using namespace ops;
 
 constexpr int TILE_MIN = 64, TILES = 512;   // rows of a tile at least; tiles at most
 constexpr int GN_COLS = 2048;       // columns of a group at most (a block's lanes hold them)
-constexpr int BLOCKS_BWD = 2048;    // blocks of the reverse pass per slab, whose column sums are folded
+// Waves of the reverse pass, whose blocks' column sums are folded: twice what is
+// resident (65,502 x 256 BF16, 1,871 samples: 51 us; with 2,048 56, 8,192 56,
+// 15,000, one per sample and slab, 79).
+constexpr int WAVES_BWD = 4096;
 
 struct GnArgs {
   long long rows;
@@ -101,7 +104,7 @@ __device__ __forceinline__ bool team_any(bool x) {
 
 // Row steps that a team of TB threads (0: within a wave) holds in registers.
 constexpr int steps_held(int tb) { return tb == 512 ? 16 : 8; }
-constexpr int steps_held_bwd(int tb) { return 8; }
+constexpr int steps_held_bwd(int tb) { return 8; }   // (beside dy and dz)
 
 struct Span {
   long long a, b;
@@ -185,9 +188,9 @@ __device__ __forceinline__ float normal_cdf(float z, float& e) {
   const float h = p * t * e;
   return z < 0.f ? h : 1.f - h;
 }
-// The kernels come by activation, so that their rows' code stays within the
-// instruction cache (with all activations in one kernel, 12,000 instructions, the
-// reverse pass of 65,502 x 256 BF16 took 71 us for @@): none and ReLU, SiLU, GELU.
+// The kernels come by activation (none and ReLU, SiLU, GELU), so that a kernel's
+// code, 46 KB in the reverse pass of BF16 with SiLU, stays within the instruction
+// cache's 64 KB.
 enum { ACT_RELU, ACT_SILU, ACT_GELU };
 
 template <int ACT, int N>
@@ -233,14 +236,13 @@ template <class F>
 __device__ __forceinline__ void longer_samples(const GnArgs& a, int blk, int blocks, long long least, F&& f) {
   for (long long s0 = blk; s0 < a.samples; s0 += 64LL * blocks) {
     const long long s = s0 + (long long)(threadIdx.x & 63) * blocks;
-    bool yes = false;
-    if (s < a.samples) {
-      const Span q = span(a, (int)s);
-      yes = q.b - q.a >= least && q.b - q.a <= a.limit;
-    }
+    Span q{0, -1};
+    if (s < a.samples) q = span(a, (int)s);
+    const bool yes = s < a.samples && q.b - q.a >= least && q.b - q.a <= a.limit;
     for (unsigned long long m = __ballot(yes); m; m &= m - 1) {
-      const int k = (int)(s0 + (long long)(__ffsll(m) - 1) * blocks);
-      f(k, span(a, k));
+      const int lane = __ffsll(m) - 1;
+      f((int)(s0 + (long long)lane * blocks),
+        Span{__builtin_amdgcn_readlane((int)q.a, lane), __builtin_amdgcn_readlane((int)q.b, lane)});
     }
   }
 }
@@ -331,11 +333,17 @@ inline Plan plan_of(bool bf16, long long rows, int cols, int groups, int samples
   const int teams = p.tb / p.team;
   long long room = LAUNCH_THREADS / 1024 / p.slabs - p.tiles;
   if (room > 65535 - p.tiles) room = 65535 - p.tiles;             // (the grid's second axis)
-  if (backward && room > BLOCKS_BWD) room = BLOCKS_BWD;
+  const long long most_bwd = WAVES_BWD / (p.tb / 64) / p.slabs;
+  if (backward && room > most_bwd) room = most_bwd > 8 ? most_bwd : 8;
   if (room < 2) room = 2;                                         // (refused: more blocks than a launch holds)
-  if (p.tb == 64 && ragged) {        // (a few where the caller says that there are none)
+  if (p.tb == 64 && ragged) {
+    // blocks for the samples that a team cannot hold, most of them without one: 16 per
+    // CU (65,502 x 256 BF16, 1,871 samples: 27.0 us; one per sample 28.7, 8 per CU
+    // 28.5); the reverse pass's half; a few where the caller says that there are none
     room = (room + 1) / 2;
-    const long long most = longest > p.team / lpr * 8 ? room : 8;
+    long long most = backward ? room : 4096 / p.slabs;
+    if (most < 8 || longest <= p.team / lpr * 8) most = 8;
+    if (most > room) most = room;
     p.l_blocks = (int)(samples < most ? samples : most);
   }
   const long long blocks = (samples + (long long)teams - 1) / teams;
