@@ -46,7 +46,12 @@ __device__ __forceinline__ void put_dx(const Rows<T, V, FULL>& o, int i, const G
                                        float m1, float m2) {
   float v[V];
 #pragma unroll
-  for (int e = 0; e < V; ++e) v[e] = rs * (d.dz[e] * g[e] - m1 - d.xh[e] * m2);
+  for (int e = 0; e < V; ++e) {
+    // (a rounded as in the sums, so that nothing is left of a set of one value)
+#pragma clang fp contract(off)
+    const float up = d.dz[e] * g[e];
+    v[e] = rs * __builtin_fmaf(-d.xh[e], m2, up - m1);
+  }
   o.put(i, v);
 }
 

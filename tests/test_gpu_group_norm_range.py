@@ -103,3 +103,20 @@ def test_more_blocks_than_a_launch_holds(rt):
     with pytest.raises(PainnError, match="blocks") as e:
         B.painn_group_norm_backward(rt.ctx, B.painn_group_norm_args(**args), p, 1 << 20, p, 1 << 20, p, p)
     assert e.value.status == -8
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("kind", ["none", "silu", "gelu"])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (700, 5), (33, 64)])
+def test_sets_of_one_value(rt, dtype, kind, rows, cols):
+    """A sample of one row, a column per group: x is its own mean and dx is 0."""
+    gen = torch.Generator().manual_seed(3)
+    x, dy = (torch.randn(rows, cols, generator=gen).to(dtype).cuda() for _ in range(2))
+    g, b = ((1 + torch.randn(cols, generator=gen)).to(dtype).cuda() for _ in range(2))
+    how = dict(offsets=torch.arange(rows + 1).int().cuda(), activation=kind)
+    y, mean, rstd = rt.group_norm(x, g, b, cols, **how)
+    assert torch.equal(mean, x.float())
+    if kind == "none":
+        assert torch.equal(y, b.expand(rows, cols))
+    dx, dg, db = rt.group_norm_backward(dy, x, g, b, mean, rstd, cols, **how)
+    assert not bool(dx.any()) and not bool(dg.any())
