@@ -127,11 +127,16 @@ __device__ __forceinline__ void team_forward(const GnArgs& a, const Place<V>& p,
   bool wild = false;
   const float count = (float)x.n * (float)a.cg;
   if (x.n > 0) {
-    const float inv = __builtin_amdgcn_rcpf(count), d = sum[0] * inv, var = sum[1] * inv - d * d;
+    // (a reciprocal and a root off by one step, and a Newton step each)
+    float inv = __builtin_amdgcn_rcpf(count);
+    inv = __builtin_fmaf(__builtin_fmaf(-count, inv, 1.f), inv, inv);
+    const float d = sum[0] * inv, var = sum[1] * inv - d * d;
     const float ve = (var > 0.f || var != var ? var : 0.f) + a.eps;
     mu = pivot + d;
-    rs = __builtin_amdgcn_rsqf(ve);         // (to one step)
-    wild = !(sum[1] < 1e38f) || d * d > ve || ve < 1e-30f || (REST && (x.n >> 10) >= NR * p.rows);
+    rs = __builtin_amdgcn_rsqf(ve);
+    rs = __builtin_fmaf(rs * 0.5f, __builtin_fmaf(-ve * rs, rs, 1.f), rs);
+    wild = !(sum[1] < 1e38f) || !(ve > 1e-30f && ve < 1e38f) || d * d > ve ||
+           (REST && (x.n >> 10) >= NR * p.rows);
   }
   if (team_any<TB>(wild)) {
     double t[2] = {0.0, 0.0};

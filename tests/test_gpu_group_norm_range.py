@@ -120,3 +120,11 @@ def test_sets_of_one_value(rt, dtype, kind, rows, cols):
         assert torch.equal(y, b.expand(rows, cols))
     dx, dg, db = rt.group_norm_backward(dy, x, g, b, mean, rstd, cols, **how)
     assert not bool(dx.any()) and not bool(dg.any())
+
+
+def test_the_largest_eps(rt):
+    """A variance and an eps whose sum leaves FP32: 1 / sqrt(1.4e38 + 3e38)."""
+    x = torch.tensor([[1.2e19], [-1.2e19]]).repeat(1, 4)
+    y, mean, rstd = run(rt, x, [2], 1, 3e38)
+    want = 1 / math.sqrt(float((x.double() ** 2).mean()) + float(torch.tensor(3e38).double()))
+    assert float((rstd - want).abs().max()) <= 8 * E32 * want and not bool(mean.any())
