@@ -417,6 +417,13 @@ painn_status painn_group_norm(painn_ctx* ctx, const painn_group_norm_args* args)
  * Errors as painn_group_norm. */
 painn_status painn_group_norm_backward(painn_ctx* ctx, const painn_group_norm_args* args, const void* dy, int64_t lddy,
                                        void* dx, int64_t lddx, void* dgamma, void* dbeta);
+/* The same with mean and rstd in another layout.  strides (host): how far
+ * mean's values of one sample and the next are apart, and of one group and the
+ * next, then rstd's, in elements; 0 is a value that they share.  NULL: as the
+ * forward writes them.  PAINN_E_ARG for a negative one. */
+painn_status painn_group_norm_backward_strided(painn_ctx* ctx, const painn_group_norm_args* args, const int64_t* strides,
+                                               const void* dy, int64_t lddy, void* dx, int64_t lddx, void* dgamma,
+                                               void* dbeta);
 
 /* A dense layer: z = x w^T + bias, y = activation(z) + residual. */
 typedef struct {

@@ -12,7 +12,7 @@ from .binding import (PAINN_BF16, PAINN_FP32, PAINN_FP64, PainnError,  # noqa: F
                       painn_adamw_create, painn_adamw_free, painn_adamw_step, painn_adamw_step_scaled, painn_adamw_steps,
                       painn_gate, painn_gate_backward, painn_gate_workspace, painn_grad_norm_clip,
                       painn_grad_norm_compute, painn_grad_norm_create, painn_grad_norm_free, painn_group_norm,
-                      painn_group_norm_backward, painn_group_norm_workspace,
+                      painn_group_norm_backward, painn_group_norm_backward_strided, painn_group_norm_workspace,
                       painn_destroy, painn_forward, painn_forward_blend, painn_forward_features,
                       painn_graph_csr, painn_graph_free, painn_grouped_linear,
                       painn_grouped_linear_backward, painn_last_error, painn_layer_norm,

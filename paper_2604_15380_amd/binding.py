@@ -21,7 +21,7 @@ EXPORTS = [
     "painn_trainer_create", "painn_trainer_step", "painn_trainer_params", "painn_trainer_free",
     "painn_layer_norm", "painn_layer_norm_backward", "painn_linear", "painn_linear_backward",
     "painn_grouped_linear", "painn_grouped_linear_backward",
-    "painn_group_norm", "painn_group_norm_backward", "painn_group_norm_workspace",
+    "painn_group_norm", "painn_group_norm_backward", "painn_group_norm_backward_strided", "painn_group_norm_workspace",
     "painn_gate", "painn_gate_backward", "painn_gate_workspace",
     "painn_grad_norm_create", "painn_grad_norm_compute", "painn_grad_norm_clip", "painn_grad_norm_free",
     "painn_adamw_create", "painn_adamw_step", "painn_adamw_step_scaled", "painn_adamw_steps", "painn_adamw_free",
@@ -72,6 +72,7 @@ _SIGS = {
     "painn_adamw_create": ([_P, _I32, _P, _P, ctypes.POINTER(_P)], ctypes.c_int),
     "painn_group_norm": ([_P, _P], ctypes.c_int),
     "painn_group_norm_backward": ([_P, _P, _P, _I64, _P, _I64, _P, _P], ctypes.c_int),
+    "painn_group_norm_backward_strided": ([_P, _P, _P, _P, _I64, _P, _I64, _P, _P], ctypes.c_int),
     "painn_group_norm_workspace": ([ctypes.c_int, _I64, _I32, _I32, _I32, _I64, _I64, _I32], _I64),
     "painn_gate": ([_P, _P], ctypes.c_int),
     "painn_gate_backward": ([_P, _P, _P, ctypes.c_double, _P, _I64], ctypes.c_int),
@@ -371,6 +372,13 @@ def painn_group_norm(ctx: int, args) -> None:
 def painn_group_norm_backward(ctx: int, args, dy: int | None, lddy: int, dx: int | None, lddx: int,
                               dgamma: int | None, dbeta: int | None) -> None:
     _check(load_library().painn_group_norm_backward(ctx, _struct_at(args), dy, lddy, dx, lddx, dgamma, dbeta), ctx)
+
+
+def painn_group_norm_backward_strided(ctx: int, args, strides, dy: int | None, lddy: int, dx: int | None, lddx: int,
+                                      dgamma: int | None, dbeta: int | None) -> None:
+    """strides: mean's by sample and by group, then rstd's."""
+    _check(load_library().painn_group_norm_backward_strided(ctx, _struct_at(args), (_I64 * 4)(*strides), dy, lddy, dx, lddx,
+                                                            dgamma, dbeta), ctx)
 
 
 def painn_group_norm_workspace(precision: int, rows: int, cols: int, groups: int, n_samples: int, sample_rows: int,

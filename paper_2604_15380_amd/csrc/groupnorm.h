@@ -27,7 +27,8 @@ struct GnArgs {
   long long ldx, lddy, ldo;
   void* out;                        // y or dx; null: no dx wanted
   float *mean, *rstd;               // forward's outputs
-  const float *mu, *rs;             // reverse pass's inputs
+  const float *mu, *rs;             // reverse pass's inputs, with strides by sample and by group
+  long long mu_s, mu_g, rs_s, rs_g;
   float eps;
   int lpg, gb, slabs;               // lanes of a group, groups of a slab (powers of 2), slabs
   int lpg_bits, lpr_bits;           // log2 of lpg and of a row's lanes, lpg gb

@@ -9,6 +9,10 @@ namespace {
 // With xh = (x - mean) rstd, dz = dy act'(xh gamma + beta) and a = dz gamma:
 //   dx = rstd (a - mean(a) - xh mean(a xh)),  dgamma = sum dz xh,  dbeta = sum dz,
 // the means over the set.
+__device__ __forceinline__ void stats_of(const GnArgs& a, int sample, int group, float& mu, float& rs) {
+  mu = a.mu[sample * a.mu_s + group * a.mu_g];
+  rs = a.rs[sample * a.rs_s + group * a.rs_g];
+}
 template <class T, int V, bool FULL, int ACT>
 struct Grads {
   float xh[V], dz[V];
@@ -68,10 +72,7 @@ __device__ __forceinline__ void team_backward(const GnArgs& a, const Place<V>& p
     ys[i] = y.get(i);
   }
   float mu = 0.f, rs = 0.f;
-  if (x.n > 0 && (FULL || p.left > 0)) {
-    mu = a.mu[(size_t)s * a.groups + p.group];
-    rs = a.rs[(size_t)s * a.groups + p.group];
-  }
+  if (x.n > 0 && (FULL || p.left > 0)) stats_of(a, s, p.group, mu, rs);
   double sum[2] = {0.0, 0.0};
   float dz[NR][V];                      // (kept for dx: 65,502 x 256 BF16 56 us, formed again 64)
 #pragma unroll
@@ -146,9 +147,8 @@ __global__ void __launch_bounds__(TB) k_group_norm_bwd(GnArgs a) {
     const int t = blk - a.l_blocks - a.f_blocks;
     long_samples(a, t, [&](int slot, int sample, const Span&, long long lo, long long hi) {
       typedef Grads<T, V, FULL, ACT> G;
-      const bool idle = !FULL && p.left <= 0;
-      const float mu = idle ? 0.f : a.mu[(size_t)sample * a.groups + p.group];
-      const float rs = idle ? 0.f : a.rs[(size_t)sample * a.groups + p.group];
+      float mu = 0.f, rs = 0.f;
+      if (FULL || p.left > 0) stats_of(a, sample, p.group, mu, rs);
       double s[2] = {0.0, 0.0};
       const Rows<T, V, FULL> x(a.x, a.ldx, p, lo, hi - lo), y(a.dy, a.lddy, p, lo, hi - lo);
       for (int i0 = 0; x.has(i0); i0 += 8) {
@@ -232,7 +232,8 @@ __global__ void __launch_bounds__(TB) k_group_norm_bwd_tiles(GnArgs a) {
     if (!FULL && p.left <= 0) return;
     const double inv = 1.0 / ((double)(q.b - q.a) * a.cg);
     const float m1 = (float)(s[0] * inv), m2 = (float)(s[1] * inv);
-    const float mu = a.mu[(size_t)sample * a.groups + p.group], rs = a.rs[(size_t)sample * a.groups + p.group];
+    float mu, rs;
+    stats_of(a, sample, p.group, mu, rs);
     float g[V], b[V];
     load_n<V>((const T*)a.gamma + p.col, p.left, g);
     load_n<V>((const T*)a.beta + p.col, p.left, b);
@@ -282,6 +283,12 @@ extern "C" {
 
 painn_status painn_group_norm_backward(painn_ctx* ctx, const painn_group_norm_args* args, const void* dy, int64_t lddy,
                                        void* dx, int64_t lddx, void* dgamma, void* dbeta) {
+  return painn_group_norm_backward_strided(ctx, args, nullptr, dy, lddy, dx, lddx, dgamma, dbeta);
+}
+
+painn_status painn_group_norm_backward_strided(painn_ctx* ctx, const painn_group_norm_args* args, const int64_t* strides,
+                                               const void* dy, int64_t lddy, void* dx, int64_t lddx, void* dgamma,
+                                               void* dbeta) {
   if (!ctx) return PAINN_E_ARG;
   ctx->err.clear();
   if (!args) return fail(ctx, PAINN_E_ARG, "null arguments");
@@ -290,6 +297,8 @@ painn_status painn_group_norm_backward(painn_ctx* ctx, const painn_group_norm_ar
                                 a.activation, a.reserved);
   if (st != PAINN_OK) return st;
   if (!dgamma != !dbeta) return fail(ctx, PAINN_E_ARG, "dgamma and dbeta are formed together");
+  for (int k = 0; strides && k < 4; ++k)
+    if (strides[k] < 0) return fail(ctx, PAINN_E_ARG, "a stride of mean or rstd is negative");
   const bool some = a.rows > 0 && a.n_samples > 0;
   if (some) {
     if (!dy || !a.x || !a.gamma || !a.beta || !a.mean || !a.rstd) return fail(ctx, PAINN_E_ARG, "null array");
@@ -310,6 +319,8 @@ painn_status painn_group_norm_backward(painn_ctx* ctx, const painn_group_norm_ar
   GnArgs g{};
   fill(g, p, a, a.workspace);
   g.dy = dy; g.lddy = lddy; g.out = dx; g.ldo = lddx; g.mu = a.mean; g.rs = a.rstd;
+  g.mu_s = strides ? strides[0] : a.groups; g.mu_g = strides ? strides[1] : 1;
+  g.rs_s = strides ? strides[2] : a.groups; g.rs_g = strides ? strides[3] : 1;
   if (!dgamma) g.part = nullptr;
   return a.precision == PAINN_FP32 ? run_bwd<float>(ctx, p, g, dgamma, dbeta) : run_bwd<b16>(ctx, p, g, dgamma, dbeta);
 }

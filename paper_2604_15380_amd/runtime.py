@@ -523,13 +523,17 @@ class Runtime:
 
     def group_norm_backward(self, dy, x, weight, bias, mean, rstd, groups, offsets=None, sample_rows=None,
                             activation="none", max_rows=None, dx=None, dweight=None, dbias=None, need_dx=True):
-        """(dx, dweight, dbias) from dy and the forward's x, mean and rstd; the
-        activation's inputs are formed again.  dx is None without need_dx and
+        """(dx, dweight, dbias) from dy and the forward's x, mean and rstd
+        ([samples, groups], of any strides); the activation's inputs are
+        formed again.  dx is None without need_dx and
         may be given as dy; its rows of no sample are left as they are."""
         import torch
         prec, act, n, c, px, ldx, pw, pb, po, samples, each = self._samples(x, weight, bias, groups, offsets, sample_rows,
                                                                            activation)
-        pm, pr = (self._whole(a, k, torch.float32, (samples, groups)) for a, k in ((mean, "mean"), (rstd, "rstd")))
+        for a, k in ((mean, "mean"), (rstd, "rstd")):
+            if a.dtype is not torch.float32 or a.device != self.device or a.shape != (samples, groups):
+                raise ValueError(f"{k} must be a float32 tensor of shape {[samples, groups]} on {self.device}, "
+                                 f"not {a.dtype} {list(a.shape)} on {a.device}")
         pd, ldd = self._rows(dy, "dy", x.dtype, n, c)
         if not need_dx:
             dx = None
@@ -543,9 +547,12 @@ class Runtime:
         need = B.painn_group_norm_workspace(prec, n, c, groups, samples, each, longest, True)
         ws = x.new_empty(need, dtype=torch.uint8) if need else None
         cur = self._enter()
-        B.painn_group_norm_backward(self.ctx, B.group_norm_args(
-            prec, act, n, c, groups, po, each, samples, 0, longest, 0.0, px, ldx, pw, pb, 0, 0, pm, pr,
-            ws.data_ptr() if need else 0, need), pd, ldd, po_, ldo, pg, pbb)
+        args = B.group_norm_args(prec, act, n, c, groups, po, each, samples, 0, longest, 0.0, px, ldx, pw, pb, 0, 0,
+                                 mean.data_ptr(), rstd.data_ptr(), ws.data_ptr() if need else 0, need)
+        if mean.is_contiguous() and rstd.is_contiguous():
+            B.painn_group_norm_backward(self.ctx, args, pd, ldd, po_, ldo, pg, pbb)
+        else:
+            B.painn_group_norm_backward_strided(self.ctx, args, mean.stride() + rstd.stride(), pd, ldd, po_, ldo, pg, pbb)
         if cur is not None:
             self._leave(cur, (dy, x, weight, bias, mean, rstd, offsets, dx, dweight, dbias, ws))
         return dx, dweight, dbias
