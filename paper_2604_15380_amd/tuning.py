@@ -289,6 +289,7 @@ class GateTuner:
         if not 0 < self.k <= self.n_heads:
             raise ValueError(f"k must be within 1 and {self.n_heads} heads, not {k}")
         self.rt, self.n_layers, self.normalize, self.balance = rt, n_layers, normalize, balance
+        self.whole = bool(normalize) or self.k == self.n_heads      # a structure's weights add up to 1
         self.dtype = torch.float32 if dtype == "fp32" else torch.bfloat16
         init = {f"blend{m}.{c}": weights[f"blend{m}.{c}"] for m in range(n_layers) for c in "wb"}
         _optimized(self, init, max_norm, lr=lr, betas=betas, eps=eps, weight_decay=weight_decay, state_bits=state_bits)
@@ -320,13 +321,22 @@ class GateTuner:
             x, xz = (y, None) if last else y
         return self.rt.gate(x, self.k, normalize=self.normalize), x, layers
 
-    @staticmethod
-    def _blend(b, gate):
-        """Energies, and the energies of the heads that were chosen (0 for none)."""
+    def _blend(self, b, gate):
+        """Energies, and what the energies of the heads that were chosen give to
+        the gate's gradient (0 for none).  Where a structure's weights add up to
+        1, a value that is taken off all its heads changes neither: the FP32
+        weights then meet the differences of the heads alone, in which total
+        energies, 1e5 times as large, leave no rounding."""
         import torch
+        none = gate.indices < 0
         e = b["heads"].gather(1, gate.indices.clamp_min(0).long())
-        e = torch.where(gate.indices < 0, torch.zeros_like(e), e)
-        return (gate.weights.double() * e).sum(1), e
+        about = e[:, :1] if self.whole else torch.zeros_like(e[:, :1])
+        e = torch.where(none, torch.zeros_like(e), e - about)
+        energies = (gate.weights.double() * e).sum(1)
+        part = e - energies[:, None] if self.whole else e
+        # (a structure without a head has no energy)
+        about = torch.where(none[:, 0], torch.zeros_like(energies), about[:, 0])
+        return about + energies, torch.where(none, torch.zeros_like(e), part)
 
     def energies(self, b):
         return self._blend(b, self._forward(b)[0])[0]
