@@ -112,9 +112,11 @@ class HeadTuner:
             raise ValueError(f"adapter_norm is layer or group, not {adapter_norm!r}")
         self.rt, self.F, self.n_heads = rt, F, n_heads
         self.n_shared, self.n_branch, self.adapter = n_shared, n_branch, adapter
-        self.groups = adapter_groups if adapter and adapter_norm == "group" else 0
-        if self.groups and (self.groups < 1 or adapter % self.groups):
-            raise ValueError(f"{adapter_groups} groups do not divide {adapter} columns")
+        self.groups = 0         # of the adapter's group norm (0: it has none)
+        if adapter and adapter_norm == "group":
+            if adapter_groups < 1 or adapter % adapter_groups:
+                raise ValueError(f"{adapter_groups} groups do not divide {adapter} columns")
+            self.groups = adapter_groups
         self.dtype = torch.float32 if dtype == "fp32" else torch.bfloat16
         init = {}
         if adapter:
