@@ -129,7 +129,7 @@ __device__ __forceinline__ int sample_of(const GnArgs& a, long long row) {
   const int lane = threadIdx.x & 63;
   int lo = 0, n = a.samples;        // among [lo, lo + n)
   while (n > 1) {
-    const int step = (n + 63) / 64, s = lane * step;
+    const int step = (n - 1) / 64 + 1, s = lane * step;     // (n may be 2^31 - 1)
     const bool before = s < n && bound(a, lo + s) <= row;
     const int k = __popcll(__ballot(before));
     const int at = k > 0 ? (k - 1) * step : 0;

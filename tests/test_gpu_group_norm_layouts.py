@@ -3,7 +3,7 @@ forward's: the same bits as with contiguous ones."""
 import pytest
 import torch
 
-from test_gpu_group_norm import DTYPES, SHAPES, check_backward, inputs
+from test_gpu_group_norm import DTYPES, SHAPES, check_backward, check_forward, inputs
 
 pytestmark = pytest.mark.gpu
 
@@ -74,3 +74,22 @@ def test_refusals(rt):
         with pytest.raises(PainnError) as e:
             B.painn_group_norm_backward_strided(rt.ctx, args, strides, p, 12, p, 12, g.data_ptr(), g.data_ptr())
         assert e.value.status == -1
+
+
+def test_as_many_samples_as_a_call_takes(rt):
+    """2^31 - 1 samples, nearly all of them empty, and one in tiles: a row's sample
+    is looked up among all of them.  (30 GB)"""
+    samples, rows, first = 2**31 - 1, 5000, 10
+    offsets = torch.full((samples + 1,), first, dtype=torch.int32, device="cuda")
+    offsets[0], offsets[-1] = 0, rows
+    gen = torch.Generator().manual_seed(95)
+    data = [torch.randn(s, generator=gen) for s in ((rows, 1), (1,), (1,), (rows, 1))]
+    x, g, b, dy = (a.cuda() for a in data)
+    got = rt.group_norm(x, g, b, 1, offsets=offsets)
+    back = rt.group_norm_backward(dy, x, g, b, got[1], got[2], 1, offsets=offsets)
+    assert not bool(got[1][1:-1].any()) and not bool(got[2][1:-1].any())
+    ends = [0, samples - 1]
+    stats = [a[ends] for a in got[1:]]
+    spans = [(0, first), (first, rows)]
+    check_forward(data, spans, 1, 1e-5, "none", [got[0]] + stats, torch.float32)
+    check_backward(data, *stats, spans, 1, "none", back, torch.float32)
