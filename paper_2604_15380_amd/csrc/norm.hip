@@ -368,7 +368,7 @@ painn_status run_norm_bwd(const NormArgs& a) {
                                                        (const T*)a.gamma, a.mu, a.rs, (T*)a.dx, a.lddx);
   }
   if (a.dgamma)
-    fold_columns<T>(ctx->stream, slices, c, part, (T*)a.dgamma, (T*)a.dbeta);
+    fold_columns<T, float>(ctx->stream, slices, c, part, (T*)a.dgamma, (T*)a.dbeta);
   prof_mark(ctx->prof, ctx->stream, KC_NORM_BWD, false);
   return launched(ctx, "layer norm reverse launch");
 }
