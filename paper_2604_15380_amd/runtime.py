@@ -180,8 +180,10 @@ class GradNorm:
     """The global norm of many tensors' gradients and clipping by it
     (painn_grad_norm_*).
 
-    The tensors are read where they were when this was made.  `outs`: where
-    clip writes, by default the gradients themselves."""
+    The tensors are read where they were when this was made: a program with
+    gradients that stay in place makes it once (it allocates a table, copies it
+    to the GPU and waits for the stream).  `outs`: where clip writes, by
+    default the gradients themselves."""
 
     def __init__(self, rt, grads, outs=None):
         grads = list(grads)
@@ -424,6 +426,16 @@ class Runtime:
                              f"not {t.dtype} {list(t.shape)} on {t.device}")
         return t.data_ptr()
 
+    def _strided(self, t, name, dtype, shape):
+        """(pointer, strides) of a tensor; no strides for a contiguous one, 0 for
+        None."""
+        if t is None:
+            return 0, None
+        if t.dtype is not dtype or t.device != self.device or t.shape != shape:
+            raise ValueError(f"{name} must be a {dtype} tensor of shape {list(shape)} on {self.device}, "
+                             f"not {t.dtype} {list(t.shape)} on {t.device}")
+        return t.data_ptr(), None if t.is_contiguous() else t.stride()
+
     def layer_norm(self, x, weight, bias, eps=1e-5, out=None):
         """(y, mean, rstd) of every row of x [rows, cols]; mean and rstd [rows]
         are FP32 and go to layer_norm_backward.  `out` may be x."""
@@ -530,10 +542,8 @@ class Runtime:
         import torch
         prec, act, n, c, px, ldx, pw, pb, po, samples, each = self._samples(x, weight, bias, groups, offsets, sample_rows,
                                                                            activation)
-        for a, k in ((mean, "mean"), (rstd, "rstd")):
-            if a.dtype is not torch.float32 or a.device != self.device or a.shape != (samples, groups):
-                raise ValueError(f"{k} must be a float32 tensor of shape {[samples, groups]} on {self.device}, "
-                                 f"not {a.dtype} {list(a.shape)} on {a.device}")
+        pm, sm = self._strided(mean, "mean", torch.float32, (samples, groups))
+        pr, sr = self._strided(rstd, "rstd", torch.float32, (samples, groups))
         pd, ldd = self._rows(dy, "dy", x.dtype, n, c)
         if not need_dx:
             dx = None
@@ -548,11 +558,12 @@ class Runtime:
         ws = x.new_empty(need, dtype=torch.uint8) if need else None
         cur = self._enter()
         args = B.group_norm_args(prec, act, n, c, groups, po, each, samples, 0, longest, 0.0, px, ldx, pw, pb, 0, 0,
-                                 mean.data_ptr(), rstd.data_ptr(), ws.data_ptr() if need else 0, need)
-        if mean.is_contiguous() and rstd.is_contiguous():
+                                 pm, pr, ws.data_ptr() if need else 0, need)
+        if sm is None and sr is None:
             B.painn_group_norm_backward(self.ctx, args, pd, ldd, po_, ldo, pg, pbb)
         else:
-            B.painn_group_norm_backward_strided(self.ctx, args, mean.stride() + rstd.stride(), pd, ldd, po_, ldo, pg, pbb)
+            B.painn_group_norm_backward_strided(self.ctx, args, (sm or (groups, 1)) + (sr or (groups, 1)), pd, ldd, po_, ldo,
+                                                pg, pbb)
         if cur is not None:
             self._leave(cur, (dy, x, weight, bias, mean, rstd, offsets, dx, dweight, dbias, ws))
         return dx, dweight, dbias

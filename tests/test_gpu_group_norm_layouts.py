@@ -93,3 +93,16 @@ def test_as_many_samples_as_a_call_takes(rt):
     spans = [(0, first), (first, rows)]
     check_forward(data, spans, 1, 1e-5, "none", [got[0]] + stats, torch.float32)
     check_backward(data, *stats, spans, 1, "none", back, torch.float32)
+
+
+def test_no_statistics(rt):
+    """Without mean or rstd a call with rows is refused by the library, and one
+    without rows does not need them."""
+    from paper_2604_15380_amd import PainnError
+    x, g, stat = torch.ones(6, 12).cuda(), torch.ones(12).cuda(), torch.ones(1, 3).cuda()
+    off = torch.tensor([0, 6], dtype=torch.int32).cuda()
+    for m, r in ((None, stat), (stat, None), (None, torch.ones(3, 1).cuda().t()), (None, None)):
+        with pytest.raises(PainnError):
+            rt.group_norm_backward(x, x, g, g, m, r, 3, offsets=off)
+    dx, dw, db = rt.group_norm_backward(x[:0], x[:0], g, g, None, None, 3, offsets=off[:1])
+    assert dx.shape == (0, 12) and not bool(dw.any()) and not bool(db.any())
