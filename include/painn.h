@@ -543,7 +543,8 @@ painn_status painn_gate_backward(painn_ctx* ctx, const painn_gate_args* args, co
  * root of the sum of all squares (in FP64), factor = max_norm / norm where the
  * norm is above max_norm, else 1; clipped gradients are g factor.  A norm of
  * infinity has the factor 0 (which makes infinite gradients NaN), a norm of NaN
- * the factor NaN. */
+ * the factor NaN.  (Nothing is added to the norm ahead of the division, as some
+ * clip with max_norm / (norm + 1e-6): the clipped norm is max_norm.) */
 typedef struct {
   int64_t n;                 /* values, >= 0 */
   const void* grad;          /* [n] */

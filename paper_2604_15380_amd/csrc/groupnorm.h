@@ -171,9 +171,12 @@ struct Rows {
 
 // The normal distribution's Phi(z), and exp(-z^2 / 2).  Half of erfc(|z| / sqrt 2)
 // as exp(-z^2 / 2) t P(t), t = 1 / (1 + 0.28 |z|), the form of Abramowitz and
-// Stegun 7.1.26 with P of degree 8 fitted to 1e-7 of itself: off by 3.4 x 2^-24 at
-// most, about half of the instructions that erff takes (147,456 x 256 FP32 with
-// GELU: 30 M vector instructions with it).
+// Stegun 7.1.26 with P of degree 8, 1.7e-7 of itself off at most.  In FP32 Phi is
+// off by 4.4 x 2^-24 at most, and by 6.5 with the hardware's reciprocal and
+// exponential a step off each (12 M arguments within 13, on the CPU); far below 0 the
+// exponent's rounding leaves z^2 / 2 x 2^-24 of Phi itself.  About half of the
+// instructions that erff takes (147,456 x 256 FP32 with GELU: 30 M vector
+// instructions with it).
 __device__ __forceinline__ float normal_cdf(float z, float& e) {
   const float u = fabsf(z), t = __builtin_amdgcn_rcpf(__builtin_fmaf(u, 0.28f, 1.f));
   float p = 0.02516147866845131f;
